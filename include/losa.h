@@ -283,6 +283,99 @@ losa_status losa_construct(const void* q, const void* k, const void* v, losa_dty
                            void* stream);
 
 /*
+ * What stands before the path: rotary positions and the norms of queries and
+ * keys, which turn a layer's projections into the tensors that the calls above
+ * read.  The inputs of these calls are views, so that slices of a fused
+ * projection are taken where they lie.
+ */
+
+/* Rows of `d` contiguous elements at data + b*batch + n*token + h*head (strides in
+   elements; b < B, n < N, h < H).  data 16-byte aligned, strides multiples of 16
+   bytes and >= 0.  An input may have stride 0 (a broadcast view); the rows of an
+   output must not overlap. */
+typedef struct {
+  void* data;
+  int64_t batch, token, head;
+} losa_view;
+
+typedef enum {
+  LOSA_PAIRS_NEIGHBOURS = 0, /* pair i is (x[2i], x[2i + 1])                             */
+  LOSA_PAIRS_HALVES = 1,     /* pair i is (x[i], x[i + rot/2]), rot = sum of axis_dim    */
+  LOSA_PAIRS_RANGE_MIN_ = -2147483647 - 1,
+  LOSA_PAIRS_RANGE_MAX_ = 2147483647
+} losa_pairs;
+
+/* Rotary positions with 1 to 4 axes (one for text, two for images, three for video:
+   time, height, width).  Axis a turns the next axis_dim[a] of the row's leading
+   rot = sum(axis_dim) dims, that is axis_dim[a]/2 consecutive pairs; dims from rot
+   on are left as they are.  axis_dim[a] even and > 0, rot a multiple of 8, <= d.
+   table  device, fp32, 16-byte aligned: for axis a, position p < axis_len[a] and
+          frequency j < axis_dim[a]/2 the cosine and sine of the angle at
+          off[a] + p*axis_dim[a] + 2j and + 1, off[a] = sum over earlier axes of
+          axis_len*axis_dim.  losa_rope_table fills one.
+   pos    device, int32: position of token n on axis a at
+          pos[b*pos_batch + a*N + n] (pos_batch 0: every batch alike).  A negative
+          position leaves the axis unturned (text tokens of a joint sequence); one
+          >= axis_len[a] has no angle and gives NaN in that axis' dims. */
+typedef struct {
+  int n_axes;
+  int axis_dim[4], axis_len[4];
+  const float* table;
+  const int32_t* pos;
+  int64_t pos_batch;
+  losa_pairs pairs;
+} losa_rotation;
+
+/*
+ * Cosines and sines of losa_rotation, on the host: angle p * base^(-2j/axis_dim[a]),
+ * computed in fp64 and rounded once.  `table` is HOST memory of `capacity` floats, at
+ * least sum(axis_len*axis_dim) of them; copy it to the device.  base > 0.
+ */
+losa_status losa_rope_table(int n_axes, const int* axis_dim, const int* axis_len, double base,
+                            float* table, int64_t capacity);
+
+/*
+ * Rotary positions of one tensor: y[b][n][h] = rotation(x[b][n][h]) for n < N, and
+ * rows N <= n < N_pad of y are 0 (the padding of the calls above).  d in {64, 128}.
+ * Computed in fp32 and rounded once.  y may be x (the same view, N_pad = N), else
+ * shares no memory with it.
+ */
+losa_status losa_rope(const losa_view* x, losa_dtype dtype, int B, int N, int N_pad, int H, int d,
+                      const losa_rotation* rot, const losa_view* y, void* stream);
+
+typedef enum {
+  LOSA_NORM_RMS = 1,   /* x / sqrt(mean(x^2) + eps) * weight + bias                      */
+  LOSA_NORM_LAYER = 2, /* (x - mean(x)) / sqrt(var(x) + eps) * weight + bias             */
+  LOSA_NORM_RANGE_MIN_ = -2147483647 - 1,
+  LOSA_NORM_RANGE_MAX_ = 2147483647
+} losa_norm_kind;
+
+/* Norms of queries and keys: over each row of d (all_heads 0; weights and biases of d
+   elements) or over a token's H*d values together (all_heads not 0; of H*d elements,
+   head by head).  Weights and biases fp32, device, 16-byte aligned, NULL for one and
+   zero.  eps finite and >= 0. */
+typedef struct {
+  losa_norm_kind kind;
+  int all_heads;
+  float eps;
+  const float *q_weight, *q_bias, *k_weight, *k_bias;
+} losa_qk_norm_args;
+
+/*
+ * Norms of queries and keys and their rotary positions in one pass, values laid out
+ * beside them: q_out = rotation(norm(q)) with H heads, k_out = rotation(norm(k)) and
+ * v_out = v with H_kv heads, each as losa_rope lays out y.  norm or rot NULL: none;
+ * v and v_out both NULL: no values.  Everything between input and output is fp32
+ * (fp32 statistics, the variance about the mean) and rounded once.  An output may be
+ * its input (the same view, N_pad = N), else shares memory with none of the others.
+ */
+losa_status losa_qk_norm_rope(const losa_view* q, const losa_view* k, const losa_view* v,
+                              losa_dtype dtype, int B, int N, int N_pad, int H, int H_kv, int d,
+                              const losa_qk_norm_args* norm, const losa_rotation* rot,
+                              const losa_view* q_out, const losa_view* k_out,
+                              const losa_view* v_out, void* stream);
+
+/*
  * Workspace bytes needed by: which = 0 losa_calibrate_mass (bf16: the suggested
  * size of its optional workspace), 1 losa_select_blocks and
  * losa_select_blocks_topk, 2 losa_sparse_attn_fwd, 3 losa_block_recall,

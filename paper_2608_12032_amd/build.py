@@ -21,7 +21,7 @@ OBJDIR = os.path.join(PKG, "_build")
 ARCH = "gfx950"
 
 SOURCES = ["calib.hip", "select.hip", "sparse_fwd.hip", "f32_path.hip", "recall.hip",
-           "noalloc.hip", "abi.cpp"]
+           "noalloc.hip", "rope.hip", "abi.cpp"]
 
 COMMON = [
     "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",

@@ -27,11 +27,37 @@ STATUS = {0: "LOSA_OK", 1: "LOSA_ERR_NULL_POINTER", 2: "LOSA_ERR_INVALID_SHAPE",
 
 EXPORTED = ("losa_calibrate_mass", "losa_select_blocks", "losa_select_blocks_topk",
             "losa_block_recall", "losa_sparse_attn_fwd", "losa_sparse_attn_fwd_noalloc",
-            "losa_construct", "losa_workspace_bytes", "losa_status_string", "losa_last_error",
+            "losa_construct", "losa_rope_table", "losa_rope", "losa_qk_norm_rope",
+            "losa_workspace_bytes", "losa_status_string", "losa_last_error",
             "losa_version")
 
 # bytes of library-held scratch behind losa_sparse_attn_fwd_noalloc (per GPU)
 NOALLOC_SCRATCH_BYTES = 128 << 20
+
+
+PAIRS = {"interleaved": 0, "halves": 1}
+NORMS = {"rms": 1, "layer": 2}
+MAX_AXES = 4
+
+
+class _View(ctypes.Structure):
+    """losa_view"""
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64),
+                ("head", ctypes.c_int64)]
+
+
+class _Rotation(ctypes.Structure):
+    """losa_rotation"""
+    _fields_ = [("n_axes", ctypes.c_int), ("axis_dim", ctypes.c_int * MAX_AXES),
+                ("axis_len", ctypes.c_int * MAX_AXES), ("table", ctypes.c_void_p),
+                ("pos", ctypes.c_void_p), ("pos_batch", ctypes.c_int64), ("pairs", ctypes.c_int)]
+
+
+class _QkNorm(ctypes.Structure):
+    """losa_qk_norm_args"""
+    _fields_ = [("kind", ctypes.c_int), ("all_heads", ctypes.c_int), ("eps", ctypes.c_float),
+                ("q_weight", ctypes.c_void_p), ("q_bias", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p), ("k_bias", ctypes.c_void_p)]
 
 
 class LosaError(RuntimeError):
@@ -60,6 +86,13 @@ def _load():
     lib.losa_sparse_attn_fwd_noalloc.restype = I
     lib.losa_construct.argtypes = [P, P, P, I, I, I, I, I, I, I, F, P, P, P, P, Z, P]
     lib.losa_construct.restype = I
+    # structures by address: a pointer to one, or None
+    lib.losa_rope_table.argtypes = [I, P, P, ctypes.c_double, P, L]
+    lib.losa_rope_table.restype = I
+    lib.losa_rope.argtypes = [P, I, I, I, I, I, I, P, P, P]
+    lib.losa_rope.restype = I
+    lib.losa_qk_norm_rope.argtypes = [P, P, P, I, I, I, I, I, I, I, P, P, P, P, P, P]
+    lib.losa_qk_norm_rope.restype = I
     lib.losa_workspace_bytes.argtypes = [I, I, I, I, I, I, I, I]
     lib.losa_workspace_bytes.restype = Z
     lib.losa_status_string.argtypes = [I]
@@ -375,6 +408,149 @@ def losa_construct(q, k, v, N: int, block_q: int, block_k: int | None = None,
     return (o, mass, lse) if want_lse else (o, mass)
 
 
+class RopeTable:
+    """Cosines and sines by axis and position, on a device: what losa_rope_table returns.
+    ``data`` fp32; ``axis_dim`` and ``axis_len`` as given."""
+
+    def __init__(self, data, axis_dim, axis_len):
+        self.data, self.axis_dim, self.axis_len = data, tuple(axis_dim), tuple(axis_len)
+
+
+def losa_rope_table(axis_dim, axis_len, base: float = 10000.0, device="cuda") -> RopeTable:
+    """Table of a rotation: axis a turns ``axis_dim[a]`` dims by positions below
+    ``axis_len[a]``, pair j of it by position * base^(-2j / axis_dim[a])."""
+    axis_dim, axis_len = [int(x) for x in axis_dim], [int(x) for x in axis_len]
+    if len(axis_dim) != len(axis_len):
+        raise ValueError("axis_dim and axis_len must have the same length")
+    n = len(axis_dim)
+    host = torch.empty(max(0, sum(a * b for a, b in zip(axis_dim, axis_len))),
+                       dtype=torch.float32)
+    ints = ctypes.c_int * max(n, 1)
+    # (a table without a float is refused: the pointer is never used)
+    st = lib.losa_rope_table(n, ints(*axis_dim), ints(*axis_len), float(base),
+                             host.data_ptr() or 16, host.numel())
+    _check(st, "losa_rope_table")
+    return RopeTable(host.to(device), axis_dim, axis_len)
+
+
+def _view(t, name, device, dtype, shape):
+    """losa_view of a [B, N, H, d] tensor whose rows of d are contiguous."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} must live on {device} (got {t.device})")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
+    sb, sn, sh, sd = t.stride()
+    if sd != 1:
+        raise ValueError(f"{name} must have contiguous rows (stride 1 in the last dim)")
+    # (a stride along one element is never used, and torch may set it to anything)
+    B, N, H, _ = t.shape
+    return _View(t.data_ptr(), sb if B > 1 else 0, sn if N > 1 else 0, sh if H > 1 else 0)
+
+
+def _rotation(table, pos, pairing, B, N, device):
+    """losa_rotation of a table and positions int32 [axes, N] or [B, axes, N]."""
+    if not isinstance(table, RopeTable):
+        raise TypeError("table must be a RopeTable (losa_rope_table)")
+    n = len(table.axis_dim)
+    _arg(table.data, "table", device, dtype=torch.float32,
+         numel=sum(a * b for a, b in zip(table.axis_dim, table.axis_len)))
+    _arg(pos, "pos", device, dtype=torch.int32)
+    if tuple(pos.shape) not in ((n, N), (B, n, N)):
+        raise ValueError(f"pos must have shape {(n, N)} or {(B, n, N)} (got {tuple(pos.shape)})")
+    if pairing not in PAIRS:
+        raise ValueError(f"pairing must be one of {tuple(PAIRS)} (got {pairing!r})")
+    ints = ctypes.c_int * MAX_AXES
+    return _Rotation(n, ints(*table.axis_dim), ints(*table.axis_len), table.data.data_ptr(),
+                     pos.data_ptr(), n * N if pos.dim() == 3 else 0, PAIRS[pairing])
+
+
+def _rows_in(t, name):
+    if not isinstance(t, torch.Tensor) or t.dim() != 4:
+        raise ValueError(f"{name} must be a [B, N, H, d] tensor")
+    return t.shape
+
+
+def _rows_out(out, name, x, n_pad):
+    """The output [B, H, n_pad, d] for x [B, N, H, d], as a view of [B, n_pad, H, d]."""
+    B, _, H, d = x.shape
+    if out is None:
+        out = torch.empty((B, H, n_pad, d), dtype=x.dtype, device=x.device)
+    if not isinstance(out, torch.Tensor) or out.dim() != 4:
+        raise ValueError(f"{name} must be a [B, H, n_pad, d] tensor")
+    return out, _view(out.transpose(1, 2), name, x.device, x.dtype, (B, n_pad, H, d))
+
+
+def losa_rope(x, table: RopeTable, pos, n_pad: int | None = None, pairing: str = "interleaved",
+              out=None):
+    """Rotary positions of x [B, N, H, d] (any strides, rows of d contiguous) ->
+    [B, H, n_pad, d], rows from N on 0.  ``pos`` int32 [axes, N] or [B, axes, N];
+    ``out`` may have any strides, and may be x's own memory."""
+    B, N, H, d = _rows_in(x, "x")
+    n_pad = N if n_pad is None else n_pad
+    dcode = _dtype_code(x)
+    xv = _view(x, "x", x.device, x.dtype, x.shape)
+    rot = _rotation(table, pos, pairing, B, N, x.device)
+    out, yv = _rows_out(out, "out", x, n_pad)
+    with torch.cuda.device(x.device):
+        st = lib.losa_rope(ctypes.addressof(xv), dcode, B, N, n_pad, H, d, ctypes.addressof(rot),
+                           ctypes.addressof(yv), _stream(x.device))
+    _check(st, "losa_rope")
+    return out
+
+
+def losa_qk_norm_rope(q, k, v=None, *, norm: str | None = "rms", over: str = "head",
+                      q_weight=None, q_bias=None, k_weight=None, k_bias=None, eps: float = 1e-6,
+                      table: RopeTable | None = None, pos=None, pairing: str = "interleaved",
+                      n_pad: int | None = None, q_out=None, k_out=None, v_out=None):
+    """Norms of q [B, N, H, d] and k [B, N, H_kv, d] over each head ("head") or all of a
+    token's heads ("all"), then their rotary positions, in one pass; v beside them ->
+    (q, k) or (q, k, v), each [B, heads, n_pad, d].  Inputs and outputs may have any
+    strides; weights and biases fp32 of d or heads * d elements."""
+    B, N, H, d = _rows_in(q, "q")
+    Hkv = _rows_in(k, "k")[2]
+    dev = q.device
+    n_pad = N if n_pad is None else n_pad
+    dcode = _dtype_code(q)
+    if over not in ("head", "all"):
+        raise ValueError(f"over must be 'head' or 'all' (got {over!r})")
+    views = [_view(q, "q", dev, q.dtype, q.shape), _view(k, "k", dev, q.dtype, (B, N, Hkv, d)),
+             None if v is None else _view(v, "v", dev, q.dtype, (B, N, Hkv, d))]
+    args = None
+    if norm is not None:
+        if norm not in NORMS:
+            raise ValueError(f"norm must be None or one of {tuple(NORMS)} (got {norm!r})")
+        for name, t, heads in (("q_weight", q_weight, H), ("q_bias", q_bias, H),
+                               ("k_weight", k_weight, Hkv), ("k_bias", k_bias, Hkv)):
+            if t is not None:
+                _arg(t, name, dev, dtype=torch.float32,
+                     shape=(d if over == "head" else heads * d,))
+        args = _QkNorm(NORMS[norm], over == "all", eps, _ptr(q_weight), _ptr(q_bias),
+                       _ptr(k_weight), _ptr(k_bias))
+    elif not (q_weight is q_bias is k_weight is k_bias is None):
+        raise ValueError("weights and biases need a norm")
+    if (table is None) != (pos is None):
+        raise ValueError("table and pos must both be given or both be None")
+    rot = None if table is None else _rotation(table, pos, pairing, B, N, dev)
+    if v is None and v_out is not None:
+        raise ValueError("v_out needs v")
+    q_out, qv = _rows_out(q_out, "q_out", q, n_pad)
+    k_out, kv = _rows_out(k_out, "k_out", k, n_pad)
+    vv = None
+    if v is not None:
+        v_out, vv = _rows_out(v_out, "v_out", v, n_pad)
+    at = lambda x: None if x is None else ctypes.addressof(x)  # noqa: E731
+    with torch.cuda.device(dev):
+        st = lib.losa_qk_norm_rope(at(views[0]), at(views[1]), at(views[2]), dcode, B, N, n_pad, H,
+                                   Hkv, d, at(args), at(rot), at(qv), at(kv), at(vv),
+                                   _stream(dev))
+    _check(st, "losa_qk_norm_rope")
+    return (q_out, k_out) if v is None else (q_out, k_out, v_out)
+
+
 # shorter aliases
 calibrate_mass = losa_calibrate_mass
 select_blocks = losa_select_blocks
@@ -383,3 +559,6 @@ block_recall = losa_block_recall
 sparse_attn_fwd = losa_sparse_attn_fwd
 sparse_attn_fwd_noalloc = losa_sparse_attn_fwd_noalloc
 construct = losa_construct
+rope_table = losa_rope_table
+rope = losa_rope
+qk_norm_rope = losa_qk_norm_rope

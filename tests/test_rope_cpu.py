@@ -1,0 +1,142 @@
+"""Rotary positions and query/key norms without a GPU: the position table, and
+what the C ABI refuses before any HIP call."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+FAKE = 0x10000  # never dereferenced: every call below fails validation first
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2608_12032_amd import losa
+    return losa
+
+
+@pytest.mark.parametrize("dims,lens,base", [
+    ((128,), (5000,), 10000.0), ((44, 42, 42), (21, 30, 52), 10000.0), ((2, 6), (1, 7), 256.0),
+    ((64,), (300_000,), 500_000.0)])
+def test_table_is_cos_sin_of_the_angles(L, dims, lens, base):
+    """Angles in fp64 and one rounding: half a step of fp32 (2^-24, values are at most
+    1) plus what an fp64 angle of up to 3e5 can be off by (2^-53 of it, a few times)."""
+    t = L.losa_rope_table(dims, lens, base, device="cpu")
+    assert t.axis_dim == dims and t.axis_len == lens and t.data.dtype == torch.float32
+    off = 0
+    for dim, n in zip(dims, lens):
+        got = t.data[off:off + n * dim].view(n, dim // 2, 2).double().numpy()
+        off += n * dim
+        j = np.arange(dim // 2)
+        angle = np.arange(n)[:, None] * np.power(base, -2.0 * j / dim)[None, :]
+        assert np.abs(got[..., 0] - np.cos(angle)).max() <= 2.0 ** -24 + 2.0 ** -31
+        assert np.abs(got[..., 1] - np.sin(angle)).max() <= 2.0 ** -24 + 2.0 ** -31
+    assert off == t.data.numel()
+
+
+@pytest.mark.parametrize("dims,lens,base,status", [
+    ((), (), 1e4, 2), ((2,) * 5, (3,) * 5, 1e4, 2), ((3,), (4,), 1e4, 2), ((0,), (4,), 1e4, 2),
+    ((4,), (0,), 1e4, 2), ((4,), (4,), 0.0, 2), ((4,), (4,), math.nan, 2), ((4,), (4,), math.inf, 2)])
+def test_table_refusals(L, dims, lens, base, status):
+    with pytest.raises(L.LosaError) as e:
+        L.losa_rope_table(dims, lens, base, device="cpu")
+    assert e.value.status == status
+
+
+def test_table_capacity(L):
+    room = (ctypes.c_float * 8)()
+    one = lambda *x: (ctypes.c_int * len(x))(*x)  # noqa: E731
+    assert L.lib.losa_rope_table(1, one(4), one(3), 1e4, room, 11) == 6
+    assert L.lib.losa_rope_table(1, one(4), one(3), 1e4, None, 12) == 1
+    # 2^31 floats: beyond the kernels' 32-bit table index
+    assert L.lib.losa_rope_table(1, one(1 << 10), one(1 << 21), 1e4, room, 1 << 40) == 2
+
+
+def rotation(L, **kw):
+    a = dict(n_axes=3, dim=(44, 42, 42, 0), len=(21, 30, 52, 0), table=FAKE, pos=FAKE, pos_batch=0,
+             pairs=0)
+    a.update(kw)
+    return L._Rotation(a["n_axes"], (ctypes.c_int * 4)(*a["dim"]), (ctypes.c_int * 4)(*a["len"]),
+                       a["table"], a["pos"], a["pos_batch"], a["pairs"])
+
+
+def view(L, data=FAKE, batch=100 * 512, token=512, head=128):
+    return L._View(data, batch, token, head)
+
+
+def rope(L, x=None, y=None, rot=None, dtype=1, B=2, N=100, N_pad=100, H=4, d=128, **kw):
+    x = view(L) if x is None else x
+    y = view(L) if y is None else y
+    rot = rotation(L, **kw) if rot is None else rot
+    at = lambda s: None if s == 0 else ctypes.addressof(s)  # noqa: E731
+    return L.lib.losa_rope(at(x), dtype, B, N, N_pad, H, d, at(rot), at(y), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(x=0), 1), (dict(y=0), 1), (dict(rot=0), 1), (dict(table=None), 1), (dict(pos=None), 1),
+    (dict(B=0), 2), (dict(N=0), 2), (dict(H=-1), 2), (dict(N_pad=99), 2), (dict(d=0), 2),
+    (dict(d=96), 5), (dict(dtype=7), 5), (dict(pairs=2), 5), (dict(n_axes=0), 2),
+    (dict(n_axes=5), 2), (dict(dim=(43, 42, 42, 0)), 2), (dict(dim=(64, 42, 42, 0)), 2),
+    (dict(dim=(42, 42, 42, 0)), 2),                         # 126: no multiple of 8
+    (dict(len=(21, 0, 52, 0)), 2), (dict(table=FAKE + 4), 4), (dict(pos=FAKE + 2), 4),
+    (dict(pos_batch=-1), 2), (dict(pos_batch=299), 2), (dict(N_pad=(1 << 30) + 1), 2),
+])
+def test_rope_refusals(L, kw, code):
+    assert rope(L, **kw) == code
+    assert L.lib.losa_last_error().decode() != ""
+
+
+@pytest.mark.parametrize("which", ["x", "y"])
+@pytest.mark.parametrize("kw,code", [
+    (dict(data=0), 1), (dict(data=FAKE + 8), 4), (dict(token=-512), 2), (dict(head=132), 4),
+    (dict(token=1 << 41), 2)])
+def test_view_refusals(L, which, kw, code):
+    assert rope(L, **{which: view(L, **kw)}) == code
+
+
+@pytest.mark.parametrize("kw", [dict(batch=0), dict(token=0), dict(head=0), dict(head=64)])
+def test_overlapping_output_rows_are_refused(L, kw):
+    assert rope(L, y=view(L, **kw)) == 2
+
+
+def norms(L, kind=1, all_heads=0, eps=1e-6, qw=None, qb=None, kw=None, kb=None):
+    return L._QkNorm(kind, all_heads, eps, qw, qb, kw, kb)
+
+
+def qkn(L, q=1, k=1, v=1, qo=1, ko=1, vo=1, norm=None, rot=1, dtype=1, H=4, Hkv=2, d=128, N_pad=100):
+    pick = lambda s: view(L) if isinstance(s, int) and s == 1 else s  # noqa: E731
+    keep = [pick(s) for s in (q, k, v, qo, ko, vo)]
+    norm = norms(L) if norm is None else norm
+    rot = rotation(L) if isinstance(rot, int) and rot == 1 else rot
+    at = lambda s: None if isinstance(s, int) and s == 0 else ctypes.addressof(s)  # noqa: E731
+    q, k, v, qo, ko, vo = (at(s) for s in keep)
+    return L.lib.losa_qk_norm_rope(q, k, v, dtype, 2, 100, N_pad, H, Hkv, d, at(norm), at(rot), qo,
+                                   ko, vo, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(q=0), 1), (dict(k=0), 1), (dict(qo=0), 1), (dict(ko=0), 1), (dict(v=0), 1),
+    (dict(vo=0), 1), (dict(Hkv=0), 2), (dict(H=0), 2), (dict(N_pad=3), 2), (dict(d=32), 5),
+    (dict(dtype=-3), 5)])
+def test_qk_norm_rope_refusals(L, kw, code):
+    assert qkn(L, **kw) == code
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(kind=0), 5), (dict(kind=3), 5), (dict(eps=-1e-6), 2), (dict(eps=math.nan), 2),
+    (dict(eps=math.inf), 2), (dict(qw=FAKE + 4), 4), (dict(kb=FAKE + 8), 4)])
+def test_norm_refusals(L, kw, code):
+    assert qkn(L, norm=norms(L, **kw)) == code
+
+
+def test_binding_refuses_host_tensors(L):
+    x = torch.zeros((1, 4, 2, 64))
+    t = L.losa_rope_table((64,), (4,), device="cpu")
+    pos = torch.zeros((1, 4), dtype=torch.int32)
+    with pytest.raises(ValueError, match="must live on"):
+        L.losa_rope(x, t, pos)
+    with pytest.raises(ValueError, match="must live on"):
+        L.losa_qk_norm_rope(x, x)
+    with pytest.raises(ValueError, match="same length"):
+        L.losa_rope_table((64,), (4, 4), device="cpu")
