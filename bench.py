@@ -108,8 +108,8 @@ def _code_only(text: str) -> str:
 # the sources of the bf16 kernels that the traffic record covers, their shared
 # headers and the C ABI that launches them (the fp32 path and the recall
 # kernels are not in the record)
-TRAFFIC_SOURCES = ("abi.cpp", "calib.hip", "common.hpp", "launch.hpp", "select.hip",
-                   "sparse_fwd.hip")
+TRAFFIC_SOURCES = ("abi.cpp", "attn_bf16.hpp", "calib.hip", "common.hpp", "launch.hpp",
+                   "select.hip", "sparse_fwd.hip")
 
 
 def source_hash() -> str:

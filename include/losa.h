@@ -376,6 +376,75 @@ losa_status losa_qk_norm_rope(const losa_view* q, const losa_view* k, const losa
                               const losa_view* v_out, void* stream);
 
 /*
+ * Attention beside the path: dense or causal attention over packed sequences of
+ * different lengths with grouped heads, for the steps before t0, text keys, prompts,
+ * and single tokens over long caches.
+ *
+ * Sequence i owns q rows q_start[i] .. + q_len[i] and k, v rows k_start[i] .. +
+ * k_len[i].  Query head h reads key head h / (H / H_kv).  Token t of a sequence sees
+ * all its keys or, causal, keys j <= t + k_len - q_len (aligned at the end: the last
+ * token sees every key).  Lengths may be 0; q_len may exceed k_len.
+ */
+
+/* What losa_packed_plan tells about a plan; the calls below read it. */
+typedef struct {
+  int64_t bytes;          /* of the plan                                                   */
+  int64_t q_rows, k_rows; /* rows that q and o, and k and v, must have                     */
+  int64_t part_rows;      /* rows of partial results (the workspace's size)                */
+  int32_t n_tiles, n_few, n_joins; /* units of work                                        */
+  int32_t H, H_kv, causal;
+  losa_dtype dtype;
+} losa_packed_info;
+
+/*
+ * The plan of a batch of packed sequences: its units of work, longest first.  A HOST
+ * function (no HIP call): the arrays and `plan` are host memory.  Copy the plan to
+ * the device and keep it as long as the lengths stay: every layer and step reads the
+ * same one.
+ *
+ * q_start, k_start  int64 [n_seq], NULL: one sequence after another.  Rows of q that
+ *                   two sequences own are refused (LOSA_ERR_INVALID_SHAPE); rows of k
+ *                   may be shared.
+ * q_len, k_len      int32 [n_seq], >= 0.  n_seq >= 0.
+ * plan              NULL: only `info` is filled.  Else at least info->bytes bytes,
+ *                   8-byte aligned.
+ * H must be a multiple of H_kv.
+ * A sequence's rows are q_len * H / H_kv per key head.  Few rows (bf16 32 or fewer, f32
+ * 16) split its keys into parts that are joined; how follows from its own lengths and
+ * H / H_kv alone, so a sequence gives the same bits alone and packed among others.
+ */
+losa_status losa_packed_plan(const int64_t* q_start, const int32_t* q_len, const int64_t* k_start,
+                             const int32_t* k_len, int n_seq, losa_dtype dtype, int H, int H_kv,
+                             int causal, void* plan, size_t plan_bytes, losa_packed_info* info);
+
+/* Workspace bytes of losa_packed_attn_fwd for this plan and head dim (0: none). */
+size_t losa_packed_workspace_bytes(const losa_packed_info* info, int d);
+
+/*
+ * O = softmax(scale Q K^T + mask) V of every sequence of the plan.
+ *
+ * q, k, v     views (batch stride unused) of q_rows x H, k_rows x H_kv rows of d, at
+ *             least info->q_rows and info->k_rows of them.  k and v: token stride
+ *             >= d, at most 64 MiB.
+ * plan        device, 8-byte aligned, what losa_packed_plan filled together with `info`.
+ * o           out, view like q: the sequences' rows.  A row that sees no key is 0.
+ *             Rows that no sequence owns are left as they are.  May be q (same view).
+ * lse         out, nullable, fp32, 4-byte aligned: natural-log logsumexp of the scaled
+ *             scores of row r and head h at lse[h*lse_head + r]; -inf where no key is
+ *             seen.  lse_head >= info->q_rows.
+ * workspace   >= losa_packed_workspace_bytes(info, d) bytes, 16-byte aligned, rewritten
+ *             by every call.
+ * Arithmetic as in losa_sparse_attn_fwd (bf16: probabilities rounded to bf16 for the
+ * P V product; f32: the normaliser of a unit carried in fp64).  Values that are not
+ * finite, at keys that a row does not see, do not reach it.
+ */
+losa_status losa_packed_attn_fwd(const losa_view* q, const losa_view* k, const losa_view* v,
+                                 int64_t q_rows, int64_t k_rows, const losa_packed_info* info,
+                                 const void* plan, int d, float scale, const losa_view* o,
+                                 float* lse, int64_t lse_head, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
  * Workspace bytes needed by: which = 0 losa_calibrate_mass (bf16: the suggested
  * size of its optional workspace), 1 losa_select_blocks and
  * losa_select_blocks_topk, 2 losa_sparse_attn_fwd, 3 losa_block_recall,

@@ -21,7 +21,8 @@ OBJDIR = os.path.join(PKG, "_build")
 ARCH = "gfx950"
 
 SOURCES = ["calib.hip", "select.hip", "sparse_fwd.hip", "f32_path.hip", "recall.hip",
-           "noalloc.hip", "rope.hip", "abi.cpp"]
+           "noalloc.hip", "rope.hip", "packed_bf16.hip", "packed_f32.hip",
+           "packed_plan.cpp", "abi.cpp", "abi_rope.cpp", "abi_packed.cpp"]
 
 COMMON = [
     "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",

@@ -8,6 +8,7 @@
 #include <cstdarg>
 #include <cstdio>
 
+#include "abi.hpp"
 #include "launch.hpp"
 
 static_assert(LOSA_NOALLOC_SCRATCH_BYTES == losa::kNoAllocScratchBytes,
@@ -17,7 +18,9 @@ namespace {
 
 thread_local char g_err[512] = "";
 
-losa_status fail(losa_status s, const char* fmt, ...) {
+}  // namespace
+
+losa_status losa::fail(losa_status s, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
@@ -25,9 +28,14 @@ losa_status fail(losa_status s, const char* fmt, ...) {
   return s;
 }
 
-bool pow2_in(int x, int lo, int hi) { return x >= lo && x <= hi && (x & (x - 1)) == 0; }
+namespace {
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+using losa::aligned16;
+using losa::elem_bytes;
+using losa::fail;
+using losa::hip_status;
+
+bool pow2_in(int x, int lo, int hi) { return x >= lo && x <= hi && (x & (x - 1)) == 0; }
 
 struct Shape {
   int B, H, N, d, bq, bk;
@@ -75,13 +83,6 @@ losa_status check_supported(losa_dtype dtype, const Shape& s) {
     return fail(LOSA_ERR_UNSUPPORTED, "block_k=%d not supported (block_q=%d, or 32)", s.bk, s.bq);
   return LOSA_OK;
 }
-
-losa_status hip_status(hipError_t e, const char* what) {
-  if (e == hipSuccess) return LOSA_OK;
-  return fail(LOSA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-size_t elem_bytes(losa_dtype dt) { return dt == LOSA_DTYPE_BF16 ? 2 : 4; }
 
 constexpr size_t kMaxLds = 160 * 1024;
 
@@ -417,209 +418,6 @@ losa_status losa_construct(const void* q, const void* k, const void* v, losa_dty
     if (st != LOSA_OK) return st;
   }
   return LOSA_OK;
-}
-
-}  // extern "C"
-
-namespace {
-
-// A view of [B][N][H] rows of d elements.  Fails on what the kernels cannot address.
-losa_status check_view(const char* name, const losa_view* v, int el, int B, int N, int H, int d,
-                       bool out) {
-  if (!v || !v->data) return fail(LOSA_ERR_NULL_POINTER, "%s must be non-NULL", name);
-  const int64_t s[3] = {v->batch, v->token, v->head};
-  const int n[3] = {B, N, H};
-  for (int i = 0; i < 3; ++i) {
-    if (s[i] < 0 || s[i] >= ((int64_t)1 << 40))
-      return fail(LOSA_ERR_INVALID_SHAPE, "%s: stride %lld out of range", name, (long long)s[i]);
-    if (s[i] * el % 16 != 0)
-      return fail(LOSA_ERR_ALIGNMENT, "%s: strides must be multiples of 16 bytes", name);
-    if (out && n[i] > 1 && s[i] < d)
-      return fail(LOSA_ERR_INVALID_SHAPE, "%s: rows of an output overlap (stride %lld < d=%d)",
-                  name, (long long)s[i], d);
-  }
-  if (!aligned16(v->data)) return fail(LOSA_ERR_ALIGNMENT, "%s must be 16-byte aligned", name);
-  return LOSA_OK;
-}
-
-losa_status check_rows(losa_dtype dtype, int B, int N, int N_pad, int H, int d) {
-  if (B <= 0 || N <= 0 || H <= 0 || d <= 0)
-    return fail(LOSA_ERR_INVALID_SHAPE, "B=%d N=%d H=%d d=%d must all be > 0", B, N, H, d);
-  if (N_pad < N) return fail(LOSA_ERR_INVALID_SHAPE, "N_pad=%d < N=%d", N_pad, N);
-  if (N_pad > (1 << 30) || H > (1 << 20))
-    return fail(LOSA_ERR_INVALID_SHAPE, "N_pad=%d or H=%d is too large", N_pad, H);
-  if (dtype != LOSA_DTYPE_F32 && dtype != LOSA_DTYPE_BF16)
-    return fail(LOSA_ERR_UNSUPPORTED, "unknown dtype %d", (int)dtype);
-  if (d != 64 && d != 128)
-    return fail(LOSA_ERR_UNSUPPORTED, "head dim d=%d not supported (64 or 128)", d);
-  return LOSA_OK;
-}
-
-// Axes of a rotation: their dims and table offsets.  d <= 0: no bound on their sum.
-losa_status check_axes(int n_axes, const int* dim, const int* len, int d, int* rot, int64_t* floats) {
-  if (n_axes < 1 || n_axes > losa::kMaxAxes)
-    return fail(LOSA_ERR_INVALID_SHAPE, "n_axes=%d not in [1, %d]", n_axes, losa::kMaxAxes);
-  int64_t sum = 0;
-  *floats = 0;
-  for (int a = 0; a < n_axes; ++a) {
-    if (dim[a] <= 0 || dim[a] % 2 != 0 || len[a] <= 0)
-      return fail(LOSA_ERR_INVALID_SHAPE, "axis %d: dim=%d must be even and > 0, len=%d > 0", a,
-                  dim[a], len[a]);
-    sum += dim[a];
-    *floats += (int64_t)dim[a] * len[a];
-    if (*floats >= ((int64_t)1 << 31))
-      return fail(LOSA_ERR_INVALID_SHAPE, "the position table exceeds the 32-bit index range");
-  }
-  if (d > 0 && (sum > d || sum % 8 != 0))
-    return fail(LOSA_ERR_INVALID_SHAPE, "axis dims sum to %lld: not a multiple of 8 up to d=%d",
-                (long long)sum, d);
-  *rot = (int)sum;
-  return LOSA_OK;
-}
-
-losa_status check_rotation(const losa_rotation* r, int N, int d, losa::RowsArgs* a) {
-  int rot = 0;
-  int64_t floats = 0;
-  const losa_status st = check_axes(r->n_axes, r->axis_dim, r->axis_len, d, &rot, &floats);
-  if (st != LOSA_OK) return st;
-  if (!r->table || !r->pos)
-    return fail(LOSA_ERR_NULL_POINTER, "the rotation's table and pos must be non-NULL");
-  if (!aligned16(r->table) || (reinterpret_cast<uintptr_t>(r->pos) & 3u) != 0)
-    return fail(LOSA_ERR_ALIGNMENT, "the rotation's table must be 16-byte, pos 4-byte aligned");
-  if (r->pos_batch < 0 || r->pos_batch >= ((int64_t)1 << 40) ||
-      (r->pos_batch != 0 && r->pos_batch < (int64_t)r->n_axes * N))
-    return fail(LOSA_ERR_INVALID_SHAPE, "pos_batch=%lld must be 0 or hold n_axes*N positions",
-                (long long)r->pos_batch);
-  if (r->pairs != LOSA_PAIRS_NEIGHBOURS && r->pairs != LOSA_PAIRS_HALVES)
-    return fail(LOSA_ERR_UNSUPPORTED, "unknown pairs %d", (int)r->pairs);
-  a->table = r->table;
-  a->pos = r->pos;
-  a->pos_batch = r->pos_batch;
-  a->axes = r->n_axes;
-  a->rot8 = rot / 8;
-  int pair = 0, off = 0;
-  for (int x = 0; x < r->n_axes; ++x) {
-    a->pair0[x] = pair;
-    a->dim[x] = r->axis_dim[x];
-    a->len[x] = r->axis_len[x];
-    a->off[x] = off;
-    pair += r->axis_dim[x] / 2;
-    off += r->axis_dim[x] * r->axis_len[x];
-  }
-  return LOSA_OK;
-}
-
-void set_tensor(losa::RowsTensor* t, const losa_view* x, const losa_view* y, int H) {
-  t->x = x->data;
-  t->xb = x->batch;
-  t->xt = x->token;
-  t->xh = x->head;
-  t->y = y->data;
-  t->yb = y->batch;
-  t->yt = y->token;
-  t->yh = y->head;
-  t->H = H;
-}
-
-}  // namespace
-
-extern "C" {
-
-losa_status losa_rope_table(int n_axes, const int* axis_dim, const int* axis_len, double base,
-                            float* table, int64_t capacity) {
-  if (!axis_dim || !axis_len || !table)
-    return fail(LOSA_ERR_NULL_POINTER, "axis_dim, axis_len and table must be non-NULL");
-  int rot = 0;
-  int64_t floats = 0;
-  const losa_status st = check_axes(n_axes, axis_dim, axis_len, 0, &rot, &floats);
-  if (st != LOSA_OK) return st;
-  if (!std::isfinite(base) || !(base > 0.0))
-    return fail(LOSA_ERR_INVALID_SHAPE, "base must be finite and > 0");
-  if (capacity < floats)
-    return fail(LOSA_ERR_CAPACITY, "capacity=%lld < %lld floats", (long long)capacity,
-                (long long)floats);
-  for (int a = 0; a < n_axes; ++a)
-    for (int p = 0; p < axis_len[a]; ++p)
-      for (int j = 0; j < axis_dim[a] / 2; ++j) {
-        const double angle = p * std::pow(base, -2.0 * j / axis_dim[a]);
-        *table++ = (float)std::cos(angle);
-        *table++ = (float)std::sin(angle);
-      }
-  return LOSA_OK;
-}
-
-losa_status losa_rope(const losa_view* x, losa_dtype dtype, int B, int N, int N_pad, int H, int d,
-                      const losa_rotation* rot, const losa_view* y, void* stream) {
-  if (!rot) return fail(LOSA_ERR_NULL_POINTER, "rot must be non-NULL");
-  losa_status st = check_rows(dtype, B, N, N_pad, H, d);
-  if (st != LOSA_OK) return st;
-  const int el = (int)elem_bytes(dtype);
-  if ((st = check_view("x", x, el, B, N, H, d, false)) != LOSA_OK) return st;
-  if ((st = check_view("y", y, el, B, N_pad, H, d, true)) != LOSA_OK) return st;
-  losa::RowsArgs a = {};
-  if ((st = check_rotation(rot, N, d, &a)) != LOSA_OK) return st;
-  a.B = B;
-  a.N = N;
-  a.n_pad = N_pad;
-  set_tensor(&a.t[0], x, y, H);
-  a.t[0].rotate = 1;
-  return hip_status(losa::launch_rows(d, dtype == LOSA_DTYPE_BF16,
-                                      rot->pairs == LOSA_PAIRS_HALVES, a, 1, false,
-                                      static_cast<hipStream_t>(stream)),
-                    "losa_rope");
-}
-
-losa_status losa_qk_norm_rope(const losa_view* q, const losa_view* k, const losa_view* v,
-                              losa_dtype dtype, int B, int N, int N_pad, int H, int H_kv, int d,
-                              const losa_qk_norm_args* norm, const losa_rotation* rot,
-                              const losa_view* q_out, const losa_view* k_out,
-                              const losa_view* v_out, void* stream) {
-  losa_status st = check_rows(dtype, B, N, N_pad, H, d);
-  if (st != LOSA_OK) return st;
-  if ((st = check_rows(dtype, B, N, N_pad, H_kv, d)) != LOSA_OK) return st;
-  const int el = (int)elem_bytes(dtype);
-  if ((st = check_view("q", q, el, B, N, H, d, false)) != LOSA_OK) return st;
-  if ((st = check_view("k", k, el, B, N, H_kv, d, false)) != LOSA_OK) return st;
-  if ((st = check_view("q_out", q_out, el, B, N_pad, H, d, true)) != LOSA_OK) return st;
-  if ((st = check_view("k_out", k_out, el, B, N_pad, H_kv, d, true)) != LOSA_OK) return st;
-  if ((v == nullptr) != (v_out == nullptr))
-    return fail(LOSA_ERR_NULL_POINTER, "v and v_out must both be given or both be NULL");
-  if (v) {
-    if ((st = check_view("v", v, el, B, N, H_kv, d, false)) != LOSA_OK) return st;
-    if ((st = check_view("v_out", v_out, el, B, N_pad, H_kv, d, true)) != LOSA_OK) return st;
-  }
-  losa::RowsArgs a = {};
-  if (rot && (st = check_rotation(rot, N, d, &a)) != LOSA_OK) return st;
-  bool all = false;
-  if (norm) {
-    if (norm->kind != LOSA_NORM_RMS && norm->kind != LOSA_NORM_LAYER)
-      return fail(LOSA_ERR_UNSUPPORTED, "unknown norm kind %d", (int)norm->kind);
-    if (!std::isfinite(norm->eps) || norm->eps < 0.f)
-      return fail(LOSA_ERR_INVALID_SHAPE, "eps must be finite and >= 0");
-    if ((norm->q_weight && !aligned16(norm->q_weight)) || (norm->q_bias && !aligned16(norm->q_bias)) ||
-        (norm->k_weight && !aligned16(norm->k_weight)) || (norm->k_bias && !aligned16(norm->k_bias)))
-      return fail(LOSA_ERR_ALIGNMENT, "norm weights and biases must be 16-byte aligned");
-    all = norm->all_heads != 0;
-  }
-  a.B = B;
-  a.N = N;
-  a.n_pad = N_pad;
-  set_tensor(&a.t[0], q, q_out, H);
-  set_tensor(&a.t[1], k, k_out, H_kv);
-  if (v) set_tensor(&a.t[2], v, v_out, H_kv);
-  a.t[0].rotate = a.t[1].rotate = rot != nullptr;
-  if (norm) {
-    a.eps = norm->eps;
-    a.t[0].norm = a.t[1].norm = norm->kind == LOSA_NORM_RMS ? losa::kNormRms : losa::kNormLayer;
-    a.t[0].w = norm->q_weight;
-    a.t[0].b = norm->q_bias;
-    a.t[1].w = norm->k_weight;
-    a.t[1].b = norm->k_bias;
-  }
-  return hip_status(losa::launch_rows(d, dtype == LOSA_DTYPE_BF16,
-                                      rot && rot->pairs == LOSA_PAIRS_HALVES, a, v ? 3 : 2, all,
-                                      static_cast<hipStream_t>(stream)),
-                    "losa_qk_norm_rope");
 }
 
 size_t losa_workspace_bytes(int which, losa_dtype dtype, int B, int H, int N, int d, int block_q,

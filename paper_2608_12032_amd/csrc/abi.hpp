@@ -1,0 +1,27 @@
+// What the files behind include/losa.h share: status reporting and argument checks.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "losa.h"
+
+namespace losa {
+
+// Sets the thread's error text and returns s.
+losa_status fail(losa_status s, const char* fmt, ...);
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+inline losa_status hip_status(hipError_t e, const char* what) {
+  if (e == hipSuccess) return LOSA_OK;
+  return fail(LOSA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+inline size_t elem_bytes(losa_dtype dt) { return dt == LOSA_DTYPE_BF16 ? 2 : 4; }
+
+// A view of [B][N][H] rows of d elements of `el` bytes.  Fails on what the kernels
+// cannot address; rows of an output must not overlap.
+losa_status check_view(const char* name, const losa_view* v, int el, int B, int64_t N, int H, int d,
+                       bool out);
+
+}  // namespace losa

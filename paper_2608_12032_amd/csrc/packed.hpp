@@ -1,0 +1,63 @@
+// Internal launchers and plan of the packed attention; arguments are checked in
+// abi_packed.cpp.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace losa {
+
+// Packed attention (packed_plan.cpp, packed_bf16.hip, packed_f32.hip).  A row of a
+// sequence is one query token under one query head of a key head's group, numbered
+// token * G + head in group, so that rows which share keys fill a tile together.
+// One unit of work: rows row0 .. of a sequence against its keys c0 .. c1.
+struct PackedItem {
+  int64_t q0, k0;        // first row of q and of k the sequence owns
+  int32_t q_len, k_len;  // its tokens
+  int32_t row0, c0, c1;
+  int32_t part;  // first partial row to write, or -1: the result itself
+};
+// One row whose keys were split: n partial rows at part, part + step, ...
+struct PackedJoin {
+  int64_t q_row;  // row of q
+  int32_t in_group, part, step, n;
+};
+struct PackedArgs {
+  const PackedItem* items;
+  const PackedJoin* joins;
+  const void *q, *k, *v;
+  void* o;
+  float* lse;
+  float *part_o, *part_ml;               // [partial row][H_kv][d], [...][2]: max (log2 units), sum
+  int64_t qt, qh, kt, kh, vt, vh, ot, oh;  // token and head strides, elements
+  int64_t lse_head;
+  int64_t q_rows, k_rows;
+  int H_kv, G, causal;
+  float scale_log2;
+};
+// Rows of a tile, rows of a sequence that make it a few-row one, keys of a part.
+constexpr int kPackedTile[2] = {32, 128};  // [bf16]
+constexpr int kPackedFew[2] = {16, 32};
+// The sequences of a call as the plan takes them (starts null: one after another).
+struct PackedSeqs {
+  const int64_t *q_start, *k_start;
+  const int32_t *q_len, *k_len;
+  int n, G, H_kv, causal;
+  bool bf16;
+};
+struct PackedCounts {
+  int tiles, few, joins;
+  int64_t part_rows;
+};
+// False: more units than a launch takes.  The plan is tiles, few-row units, joins.
+bool packed_counts(const PackedSeqs& s, PackedCounts* out);
+void packed_fill(const PackedSeqs& s, const PackedCounts& n, void* plan);
+inline size_t packed_plan_bytes(const PackedCounts& n) {
+  return ((size_t)n.tiles + n.few) * sizeof(PackedItem) + (size_t)n.joins * sizeof(PackedJoin);
+}
+hipError_t launch_packed_bf16(int d, const PackedArgs& a, int n_tiles, int n_few, hipStream_t stream);
+hipError_t launch_packed_f32(int d, const PackedArgs& a, int n_tiles, int n_few, hipStream_t stream);
+hipError_t launch_packed_join(int d, bool bf16, const PackedArgs& a, int n_joins, hipStream_t stream);
+
+}  // namespace losa

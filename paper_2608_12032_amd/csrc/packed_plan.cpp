@@ -1,0 +1,116 @@
+// Units of work of the packed attention, laid out on the host from the sequences'
+// lengths, which a program knows there.  Everything about a sequence's split follows
+// from its own lengths and the group size, never from the batch around it, so it gives
+// the same bits alone and packed among others.
+#include <algorithm>
+
+#include "packed.hpp"
+
+namespace losa {
+
+namespace {
+
+// Keys of a part of a few-row sequence (a multiple of the 32-key sub-tile).
+// bf16: a part is one wave.  128 keys at least, so that a part's partial rows stay
+// small beside its K and V; 256 parts at most, so that the join stays short.  fp32: a
+// part is a workgroup of eight waves, two sub-tiles each at least.
+int part_keys(bool bf16, int k_len) {
+  const int least = bf16 ? 128 : 512;
+  const int64_t even = ((int64_t)k_len + 255) / 256;
+  const int64_t keys = (even + 63) / 64 * 64;
+  return (int)(keys < least ? least : keys);
+}
+
+struct Counts {
+  int64_t tiles, few, joins, part_rows;
+};
+
+// Calls tile(item), few(item), join(row) for every unit, in order; returns their number.
+template <typename Tile, typename Few, typename Join>
+Counts walk(const PackedSeqs& s, Tile&& tile, Few&& few, Join&& join) {
+  Counts c = {0, 0, 0, 0};
+  int64_t q0 = 0, k0 = 0;
+  const int block = kPackedTile[s.bf16];
+  for (int i = 0; i < s.n; ++i) {
+    PackedItem it = {};
+    it.q0 = s.q_start ? s.q_start[i] : q0;
+    it.k0 = s.k_start ? s.k_start[i] : k0;
+    it.q_len = s.q_len[i];
+    it.k_len = s.k_len[i];
+    q0 += it.q_len;
+    k0 += it.k_len;
+    it.part = -1;
+    const int64_t rows = (int64_t)it.q_len * s.G;
+    if (rows == 0) continue;
+    if (rows > kPackedFew[s.bf16]) {
+      for (int64_t r = 0; r < rows; r += block) {
+        it.row0 = (int)r;
+        it.c0 = 0;
+        it.c1 = it.k_len;
+        if (s.causal) {
+          // the last row's last key
+          const int64_t tok = std::min<int64_t>(it.q_len - 1, (r + block - 1) / s.G);
+          it.c1 = (int)std::max<int64_t>(0, std::min<int64_t>(it.k_len, tok + it.k_len - it.q_len + 1));
+        }
+        tile(it);
+        ++c.tiles;
+      }
+      continue;
+    }
+    const int keys = part_keys(s.bf16, it.k_len);
+    const int parts = std::max(1, (int)(((int64_t)it.k_len + keys - 1) / keys));
+    for (int p = 0; p < parts; ++p) {
+      it.row0 = 0;
+      it.c0 = p * keys;
+      it.c1 = std::min(it.k_len, it.c0 + keys);
+      if (parts > 1) it.part = (int)(c.part_rows + p * rows);
+      few(it);
+      ++c.few;
+    }
+    if (parts > 1) {
+      for (int64_t r = 0; r < rows; ++r) {
+        join(PackedJoin{it.q0 + r / s.G, (int)(r % s.G), (int)(c.part_rows + r), (int)rows, parts});
+        ++c.joins;
+      }
+      c.part_rows += parts * rows;
+      if (c.part_rows >= ((int64_t)1 << 31)) break;
+    }
+  }
+  return c;
+}
+
+}  // namespace
+
+bool packed_counts(const PackedSeqs& s, PackedCounts* out) {
+  const Counts c = walk(s, [](const PackedItem&) {}, [](const PackedItem&) {},
+                        [](const PackedJoin&) {});
+  const int64_t most = ((int64_t)1 << 31) / s.H_kv - 1;
+  if (c.tiles > most || c.few > most || c.joins > most || c.part_rows >= ((int64_t)1 << 31))
+    return false;
+  out->tiles = (int)c.tiles;
+  out->few = (int)c.few;
+  out->joins = (int)c.joins;
+  out->part_rows = c.part_rows;
+  return true;
+}
+
+void packed_fill(const PackedSeqs& s, const PackedCounts& n, void* plan) {
+  PackedItem* const tiles = static_cast<PackedItem*>(plan);
+  PackedItem* const few = tiles + n.tiles;
+  PackedJoin* const joins = reinterpret_cast<PackedJoin*>(few + n.few);
+  int64_t t = 0, f = 0, j = 0;
+  walk(s, [&](const PackedItem& x) { tiles[t++] = x; }, [&](const PackedItem& x) { few[f++] = x; },
+       [&](const PackedJoin& x) { joins[j++] = x; });
+  // longest first, so that the launch's tail is made of short units; order changes only
+  // the schedule.  (std::sort: no allocation)
+  auto longer = [](const PackedItem& a, const PackedItem& b) {
+    const int la = a.c1 - a.c0, lb = b.c1 - b.c0;
+    if (la != lb) return la > lb;
+    if (a.q0 != b.q0) return a.q0 < b.q0;
+    return a.row0 != b.row0 ? a.row0 < b.row0 : a.c0 < b.c0;
+  };
+  std::sort(tiles, tiles + n.tiles, longer);
+  std::sort(few, few + n.few, longer);
+}
+
+}  // namespace losa

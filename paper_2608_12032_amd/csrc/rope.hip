@@ -20,7 +20,7 @@
 // a head (head-major attention layout): a wave's load takes whole rows, its store 1
 // KiB (bf16) in one run.
 #include "common.hpp"
-#include "launch.hpp"
+#include "rope.hpp"
 
 namespace losa {
 

@@ -2,8 +2,8 @@
 
     python -m paper_2608_12032_amd.hostsan
 
-Builds a copy of the library whose host code (abi.cpp: argument checks,
-workspace sizing, error strings) carries AddressSanitizer and
+Builds a copy of the library whose host code (the .cpp files: argument checks,
+workspace sizing, plans and tables, error strings) carries AddressSanitizer and
 UndefinedBehaviorSanitizer, linked with the kernel objects of the last
 regular build (the GPU code is not instrumented), then runs the CPU tests of
 the ABI against that copy in a child process with the ASan runtime preloaded.
@@ -21,6 +21,7 @@ from . import build as B
 
 SAN_DIR = os.path.join(B.OBJDIR, "hostsan")
 SAN_LIB = os.path.join(SAN_DIR, "liblosa.so")
+HOST = [s for s in B.SOURCES if s.endswith(".cpp")]
 # -Xarch_host before each -fsanitize= keeps the device code uninstrumented
 SAN = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
        "-Xarch_host", "-fno-omit-frame-pointer", "-Xarch_host", "-fno-sanitize-recover=all"]
@@ -37,17 +38,19 @@ def _asan_runtime() -> str:
 
 def build_sanitized() -> str:
     kernels = [os.path.join(B.OBJDIR, os.path.splitext(s)[0] + ".o")
-               for s in B.SOURCES if s != "abi.cpp"]
+               for s in B.SOURCES if s not in HOST]
     missing = [o for o in kernels if not os.path.exists(o)]
     if missing:
         raise RuntimeError("kernel objects missing; run `python -m paper_2608_12032_amd.build` "
                            "first: " + ", ".join(missing))
     os.makedirs(SAN_DIR, exist_ok=True)
     hipcc = B._hipcc()
-    abi_obj = os.path.join(SAN_DIR, "abi.o")
-    B._run([hipcc, *B.COMMON, *SAN, "-c", os.path.join(B.CSRC, "abi.cpp"), "-o", abi_obj])
+    objs = []
+    for src in HOST:
+        objs.append(os.path.join(SAN_DIR, os.path.splitext(src)[0] + ".o"))
+        B._run([hipcc, *B.COMMON, *SAN, "-c", os.path.join(B.CSRC, src), "-o", objs[-1]])
     B._run([hipcc, f"--offload-arch={B.ARCH}", "-shared", "-fPIC", *SAN, "-o", SAN_LIB,
-            *kernels, abi_obj])
+            *kernels, *objs])
     return SAN_LIB
 
 
@@ -58,9 +61,9 @@ def main() -> int:
     env["ASAN_OPTIONS"] = "detect_leaks=0:halt_on_error=1"
     env["UBSAN_OPTIONS"] = "print_stacktrace=1:halt_on_error=1"
     env["LOSA_LIBRARY"] = lib
-    tests = os.path.join(B.ROOT, "tests", "test_abi_cpu.py")
+    tests = [os.path.join(B.ROOT, "tests", f"test_{x}_cpu.py") for x in ("abi", "rope", "packed")]
     p = subprocess.run([sys.executable, "-m", "pytest", "-q", "-m", "not gpu", "-p",
-                        "no:cacheprovider", tests], env=env, cwd=B.ROOT)
+                        "no:cacheprovider", *tests], env=env, cwd=B.ROOT)
     return p.returncode
 
 

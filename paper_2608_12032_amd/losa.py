@@ -28,6 +28,7 @@ STATUS = {0: "LOSA_OK", 1: "LOSA_ERR_NULL_POINTER", 2: "LOSA_ERR_INVALID_SHAPE",
 EXPORTED = ("losa_calibrate_mass", "losa_select_blocks", "losa_select_blocks_topk",
             "losa_block_recall", "losa_sparse_attn_fwd", "losa_sparse_attn_fwd_noalloc",
             "losa_construct", "losa_rope_table", "losa_rope", "losa_qk_norm_rope",
+            "losa_packed_plan", "losa_packed_workspace_bytes", "losa_packed_attn_fwd",
             "losa_workspace_bytes", "losa_status_string", "losa_last_error",
             "losa_version")
 
@@ -58,6 +59,14 @@ class _QkNorm(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int), ("all_heads", ctypes.c_int), ("eps", ctypes.c_float),
                 ("q_weight", ctypes.c_void_p), ("q_bias", ctypes.c_void_p),
                 ("k_weight", ctypes.c_void_p), ("k_bias", ctypes.c_void_p)]
+
+
+class _PackedInfo(ctypes.Structure):
+    """losa_packed_info"""
+    _fields_ = [("bytes", ctypes.c_int64), ("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64),
+                ("part_rows", ctypes.c_int64), ("n_tiles", ctypes.c_int32),
+                ("n_few", ctypes.c_int32), ("n_joins", ctypes.c_int32), ("H", ctypes.c_int32),
+                ("H_kv", ctypes.c_int32), ("causal", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 class LosaError(RuntimeError):
@@ -93,6 +102,12 @@ def _load():
     lib.losa_rope.restype = I
     lib.losa_qk_norm_rope.argtypes = [P, P, P, I, I, I, I, I, I, I, P, P, P, P, P, P]
     lib.losa_qk_norm_rope.restype = I
+    lib.losa_packed_plan.argtypes = [P, P, P, P, I, I, I, I, I, P, Z, P]
+    lib.losa_packed_plan.restype = I
+    lib.losa_packed_workspace_bytes.argtypes = [P, I]
+    lib.losa_packed_workspace_bytes.restype = Z
+    lib.losa_packed_attn_fwd.argtypes = [P, P, P, L, L, P, P, I, F, P, P, L, P, Z, P]
+    lib.losa_packed_attn_fwd.restype = I
     lib.losa_workspace_bytes.argtypes = [I, I, I, I, I, I, I, I]
     lib.losa_workspace_bytes.restype = Z
     lib.losa_status_string.argtypes = [I]
@@ -551,6 +566,110 @@ def losa_qk_norm_rope(q, k, v=None, *, norm: str | None = "rms", over: str = "he
     return (q_out, k_out) if v is None else (q_out, k_out, v_out)
 
 
+class PackedPlan:
+    """Plan of a batch of packed sequences on a device: what losa_packed_plan returns.
+    ``info`` holds its sizes (losa_packed_info), ``data`` the units of work."""
+
+    def __init__(self, info, data, dtype):
+        self.info, self.data, self.dtype = info, data, dtype
+        self.q_rows, self.k_rows = info.q_rows, info.k_rows
+        self.heads, self.kv_heads = info.H, info.H_kv
+        self._at = ctypes.addressof(info)
+
+    def workspace_bytes(self, d: int) -> int:
+        return int(lib.losa_packed_workspace_bytes(self._at, d))
+
+    def workspace(self, d: int):
+        """A workspace for losa_packed_attn_fwd at head dim d, None where it needs none."""
+        need = self.workspace_bytes(d)
+        return torch.empty(need, dtype=torch.uint8, device=self.data.device) if need else None
+
+
+def losa_packed_plan(q_lens, k_lens, heads: int, kv_heads: int, dtype, causal: bool = False,
+                     q_starts=None, k_starts=None, device="cuda") -> PackedPlan:
+    """Plan of sequences of ``q_lens`` query tokens over ``k_lens`` keys (None: the same),
+    one after another in q and k or at ``q_starts`` and ``k_starts``.  Lengths and starts
+    are host integers.  Keep the plan for every layer and step with these lengths."""
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"unsupported dtype {dtype}")
+    q_lens = [int(x) for x in q_lens]
+    k_lens = q_lens if k_lens is None else [int(x) for x in k_lens]
+    n = len(q_lens)
+    arrays = []
+    for name, x, kind in (("q_starts", q_starts, ctypes.c_int64), ("q_lens", q_lens, ctypes.c_int32),
+                          ("k_starts", k_starts, ctypes.c_int64), ("k_lens", k_lens, ctypes.c_int32)):
+        if x is not None:
+            x = [int(y) for y in x]
+            if len(x) != n:
+                raise ValueError(f"{name} has {len(x)} entries, q_lens {n}")
+            if any(abs(y) > 2 ** 31 - 1 for y in x) and kind is ctypes.c_int32:
+                raise ValueError(f"{name} holds a length beyond 32 bits")
+            x = (kind * max(n, 1))(*x)
+        arrays.append(x)
+    code = LOSA_DTYPE_BF16 if dtype == torch.bfloat16 else LOSA_DTYPE_F32
+    info = _PackedInfo()
+
+    def call(plan, room):
+        _check(lib.losa_packed_plan(*arrays, n, code, heads, kv_heads, int(causal), plan, room,
+                                    ctypes.addressof(info)), "losa_packed_plan")
+
+    call(None, 0)
+    host = torch.empty(max(1, info.bytes // 8), dtype=torch.int64)
+    call(host.data_ptr(), host.numel() * 8)
+    return PackedPlan(info, host.to(device), dtype)
+
+
+def _packed_view(t, name, device, dtype, heads, d):
+    """losa_view of a [rows, heads, d] tensor whose rows of d are contiguous."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise ValueError(f"{name} must be a [rows, heads, d] tensor")
+    return _view(t[None], name, device, dtype, (1, t.shape[0], heads, d))
+
+
+def losa_packed_attn_fwd(q, k, v, plan: PackedPlan, scale: float | None = None,
+                         want_lse: bool = False, out=None, lse=None, workspace=None):
+    """Attention over the plan's sequences: q [rows, heads, d], k and v [rows, kv_heads, d]
+    (any strides, rows of d contiguous) -> o like q (and lse fp32 [heads, rows]).  Rows
+    of ``out`` and ``lse`` that no sequence owns are left as they are."""
+    if not isinstance(plan, PackedPlan):
+        raise TypeError("plan must be a PackedPlan (losa_packed_plan)")
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a [rows, heads, d] tensor")
+    dev, d = q.device, q.shape[2]
+    if plan.data.device != dev:
+        raise ValueError(f"the plan must live on {dev} (got {plan.data.device})")
+    rows = q.shape[0]
+    qv = _packed_view(q, "q", dev, plan.dtype, plan.heads, d)
+    kv = _packed_view(k, "k", dev, plan.dtype, plan.kv_heads, d)
+    vv = _packed_view(v, "v", dev, plan.dtype, plan.kv_heads, d)
+    if k.shape[0] != v.shape[0]:
+        raise ValueError(f"k has {k.shape[0]} rows, v {v.shape[0]}")
+    if out is None:
+        out = torch.empty((rows, plan.heads, d), dtype=q.dtype, device=dev)
+    ov = _packed_view(out, "out", dev, plan.dtype, plan.heads, d)
+    if out.shape[0] != rows:
+        raise ValueError(f"out must have shape {tuple(q.shape)} (got {tuple(out.shape)})")
+    if want_lse and lse is None:
+        lse = torch.empty((plan.heads, rows), dtype=torch.float32, device=dev)
+    if want_lse:
+        _arg(lse, "lse", dev, dtype=torch.float32, shape=(plan.heads, rows))
+    need = plan.workspace_bytes(d)
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    if workspace is not None:
+        _arg(workspace, "workspace", dev, nbytes=need)
+    ws_bytes = 0 if workspace is None else workspace.nbytes
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    at = ctypes.addressof
+    with torch.cuda.device(dev):
+        st = lib.losa_packed_attn_fwd(at(qv), at(kv), at(vv), rows, k.shape[0], plan._at,
+                                      plan.data.data_ptr(), d, scale, at(ov),
+                                      _ptr(lse if want_lse else None), rows, _ptr(workspace),
+                                      ws_bytes, _stream(dev))
+    _check(st, "losa_packed_attn_fwd")
+    return (out, lse) if want_lse else out
+
+
 # shorter aliases
 calibrate_mass = losa_calibrate_mass
 select_blocks = losa_select_blocks
@@ -562,3 +681,5 @@ construct = losa_construct
 rope_table = losa_rope_table
 rope = losa_rope
 qk_norm_rope = losa_qk_norm_rope
+packed_plan = losa_packed_plan
+packed_attn_fwd = losa_packed_attn_fwd

@@ -1,0 +1,190 @@
+"""The plan of the packed attention without a GPU (its units cover every row and key
+once, whatever the batch), and what the C ABI refuses before any HIP call."""
+import ctypes
+import random
+
+import numpy as np
+import pytest
+import torch
+
+FAKE = 0x10000  # never dereferenced: every call below fails validation first
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2608_12032_amd import losa
+    return losa
+
+
+ITEM = np.dtype([("q0", "<i8"), ("k0", "<i8"), ("q_len", "<i4"), ("k_len", "<i4"), ("row0", "<i4"),
+                 ("c0", "<i4"), ("c1", "<i4"), ("part", "<i4")])
+JOIN = np.dtype([("q_row", "<i8"), ("in_group", "<i4"), ("part", "<i4"), ("step", "<i4"), ("n", "<i4")])
+
+
+def units(plan):
+    raw = plan.data.numpy().tobytes()[:plan.info.bytes]
+    n = plan.info.n_tiles + plan.info.n_few
+    items = np.frombuffer(raw[:n * ITEM.itemsize], ITEM)
+    return items[:plan.info.n_tiles], items[plan.info.n_tiles:], np.frombuffer(raw[n * ITEM.itemsize:], JOIN)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("seed", range(6))
+def test_units_cover_every_row_and_key_once(L, dtype, causal, seed):
+    rng = random.Random(seed)
+    G = rng.choice([1, 2, 3, 8])
+    ql = [rng.choice([0, 1, 2, 5, 33, 128, 129, 400]) for _ in range(7)]
+    kl = [rng.choice([0, 1, 63, 128, 129, 700, 5000, 50_000]) for _ in ql]
+    p = L.losa_packed_plan(ql, kl, 2 * G, 2, dtype, causal=causal, device="cpu")
+    tiles, few, joins = units(p)
+    block, most = (128, 32) if dtype == torch.bfloat16 else (32, 16)
+    assert p.q_rows == max([0] + [sum(ql[:i + 1]) for i in range(7) if ql[i]])
+    parts = []
+    q0 = k0 = 0
+    for q, k in zip(ql, kl):
+        rows = q * G
+        mine = [x for x in tiles if x["q0"] == q0 and x["q_len"] == q and q] if rows > most else []
+        split = [x for x in few if x["q0"] == q0 and x["q_len"] == q] if 0 < rows <= most else []
+        for x in list(mine) + list(split):
+            assert x["k0"] == k0 and x["k_len"] == k
+        if rows > most:
+            assert sorted(x["row0"] for x in mine) == list(range(0, rows, block))
+            for x in mine:
+                last = min(q - 1, (int(x["row0"]) + block - 1) // G)
+                assert x["c0"] == 0 and x["part"] == -1
+                assert x["c1"] == (max(0, min(k, last + k - q + 1)) if causal else k)
+        elif rows:
+            split = sorted(split, key=lambda x: x["c0"])
+            edges = [(int(x["c0"]), int(x["c1"])) for x in split]
+            assert edges[0][0] == 0 and edges[-1][1] == k
+            assert all(a[1] == b[0] for a, b in zip(edges, edges[1:])) and len(edges) <= 256
+            if len(split) == 1:
+                assert split[0]["part"] == -1
+            else:
+                first = int(split[0]["part"])
+                assert [int(x["part"]) for x in split] == [first + i * rows for i in range(len(split))]
+                got = [j for j in joins if q0 <= j["q_row"] < q0 + q]
+                assert sorted((int(j["q_row"]) - q0) * G + int(j["in_group"]) for j in got) == list(range(rows))
+                for j in got:
+                    r = (int(j["q_row"]) - q0) * G + int(j["in_group"])
+                    assert (j["part"], j["step"], j["n"]) == (first + r, rows, len(split))
+                parts.append((first, first + len(split) * rows))
+        q0, k0 = q0 + q, k0 + k
+    parts.sort()
+    assert sum(b - a for a, b in parts) == p.info.part_rows
+    assert all(a[1] == b[0] for a, b in zip(parts, parts[1:]))
+    for x in (tiles, few):  # longest first
+        n = [int(y["c1"]) - int(y["c0"]) for y in x]
+        assert n == sorted(n, reverse=True)
+    assert p.workspace_bytes(128) == p.info.part_rows * 2 * 130 * 4
+
+
+def test_a_sequence_is_split_alike_in_any_batch(L):
+    alone = units(L.losa_packed_plan([3], [9000], 8, 2, torch.bfloat16, device="cpu"))[1]
+    among = units(L.losa_packed_plan([500, 3, 1], [20, 9000, 40_000], 8, 2, torch.bfloat16, device="cpu"))[1]
+    cut = lambda x: sorted((int(y["c0"]), int(y["c1"])) for y in x if y["k_len"] == 9000)  # noqa: E731
+    assert cut(alone) == cut(among)
+
+
+def test_nothing_to_do(L):
+    p = L.losa_packed_plan([], [], 4, 4, torch.float32, device="cpu")
+    assert (p.info.bytes, p.q_rows, p.k_rows, p.workspace_bytes(64)) == (0, 0, 0, 0)
+    p = L.losa_packed_plan([0, 0], [5, 0], 4, 4, torch.bfloat16, causal=True, device="cpu")
+    assert p.info.bytes == 0 and p.k_rows == 0
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(heads=0), 2), (dict(kv_heads=0), 2), (dict(heads=5, kv_heads=2), 2),
+    (dict(q_lens=[3, -1]), 2), (dict(k_lens=[3, -1]), 2), (dict(k_starts=[0, -4]), 2),
+    (dict(q_starts=[0, 2]), 2),                     # rows 2 of q belong to both
+    (dict(q_starts=[7, 5]), 2), (dict(q_lens=[1 << 30, 1 << 30], heads=4, kv_heads=2), 2),
+    (dict(q_starts=[0, 1 << 41]), 2), (dict(q_lens=[(1 << 30) + 1, 3]), 2),
+    # more workgroups than a launch takes
+    (dict(q_lens=[1 << 30, 3], heads=1 << 9, kv_heads=1 << 9), 2)])
+def test_plan_refusals(L, kw, status):
+    args = dict(q_lens=[3, 3], k_lens=[5, 5], heads=4, kv_heads=2, dtype=torch.bfloat16, device="cpu")
+    args.update(kw)
+    with pytest.raises(L.LosaError) as e:
+        L.losa_packed_plan(**args)
+    assert e.value.status == status and str(e.value)
+
+
+def test_plan_argument_checks(L):
+    with pytest.raises(TypeError, match="dtype"):
+        L.losa_packed_plan([1], [1], 1, 1, torch.float16, device="cpu")
+    with pytest.raises(ValueError, match="entries"):
+        L.losa_packed_plan([1], [1, 2], 1, 1, torch.float32, device="cpu")
+    with pytest.raises(ValueError, match="32 bits"):
+        L.losa_packed_plan([1 << 31], [1], 1, 1, torch.float32, device="cpu")
+    info = L._PackedInfo()
+    one = (ctypes.c_int32 * 1)(4)
+    call = lambda **k: L.lib.losa_packed_plan(  # noqa: E731
+        None, k.get("q", one), None, one, k.get("n", 1), k.get("dtype", 1), 2, 1, 0, k.get("plan"),
+        k.get("room", 0), k.get("info", ctypes.addressof(info)))
+    assert call() == 0 and info.bytes == ITEM.itemsize
+    assert call(info=None) == 1 and call(q=None) == 1 and call(n=-1) == 2 and call(dtype=9) == 5
+    room = (ctypes.c_int64 * 8)()
+    at = ctypes.addressof(room)
+    assert call(plan=at, room=ITEM.itemsize - 1) == 6 and call(plan=at + 4, room=64) == 4
+    assert call(plan=at, room=64) == 0
+
+
+def view(L, data=FAKE, token=512, head=128):
+    return L._View(data, 0, token, head)
+
+
+def fwd(L, q=1, k=1, v=1, o=1, q_rows=40, k_rows=4000, plan=FAKE, d=128, scale=0.1, lse=None,
+        lse_head=40, ws=FAKE, wsb=1 << 30, info=None, dtype=torch.bfloat16, lens=([4, 30], [3000, 30])):
+    if info is None:
+        info = L.losa_packed_plan(*lens, 4, 2, dtype, device="cpu").info
+    q, k, v, o = (view(L) if isinstance(x, int) and x == 1 else x for x in (q, k, v, o))
+    at = lambda x: None if isinstance(x, int) else ctypes.addressof(x)  # noqa: E731
+    return L.lib.losa_packed_attn_fwd(at(q), at(k), at(v), q_rows, k_rows, at(info), plan, d, scale,
+                                      at(o), lse, lse_head, ws, wsb, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(q=0), 1), (dict(k=0), 1), (dict(v=0), 1), (dict(o=0), 1), (dict(info=0), 1),
+    (dict(plan=None), 1), (dict(plan=FAKE + 4), 4), (dict(q_rows=33), 2), (dict(k_rows=3029), 2),
+    (dict(d=0), 2), (dict(d=96), 5), (dict(scale=0.0), 2), (dict(scale=float("nan")), 2),
+    (dict(scale=float("inf")), 2), (dict(lse=FAKE + 2), 4), (dict(lse=FAKE, lse_head=33), 2),
+    (dict(ws=None), 1), (dict(ws=FAKE + 8), 4), (dict(wsb=100), 6)])
+def test_forward_refusals(L, kw, code):
+    assert fwd(L, **kw) == code
+    assert L.lib.losa_last_error().decode() != ""
+
+
+@pytest.mark.parametrize("which", ["q", "k", "v", "o"])
+@pytest.mark.parametrize("kw,code", [(dict(data=0), 1), (dict(data=FAKE + 8), 4), (dict(token=516), 4),
+                                     (dict(head=-128), 2)])
+def test_forward_view_refusals(L, which, kw, code):
+    assert fwd(L, **{which: view(L, **kw)}) == code
+
+
+def test_forward_stride_refusals(L):
+    assert fwd(L, o=view(L, token=64)) == 2 and fwd(L, o=view(L, head=0)) == 2
+    for which in "kv":
+        assert fwd(L, **{which: view(L, token=64)}) == 2
+        assert fwd(L, **{which: view(L, token=(1 << 25) + 8)}) == 2
+
+
+def test_forward_refuses_what_is_no_info(L):
+    info = L.losa_packed_plan([4], [300], 4, 2, torch.bfloat16, device="cpu").info
+    for name, value in (("H", 5), ("H_kv", 0), ("n_tiles", 3), ("bytes", 8), ("dtype", 4), ("n_few", -1)):
+        bad = L._PackedInfo.from_buffer_copy(info)
+        setattr(bad, name, value)
+        assert fwd(L, info=bad) == 2, name
+
+
+def test_forward_of_nothing_launches_nothing(L):
+    assert fwd(L, lens=([0, 0], [5, 0]), plan=None, q_rows=0, k_rows=0, ws=None, wsb=0) == 0
+
+
+def test_binding_refuses_host_tensors(L):
+    p = L.losa_packed_plan([4], [4], 2, 1, torch.float32, device="cpu")
+    q = torch.zeros(4, 2, 64)
+    with pytest.raises(ValueError, match="must live on"):
+        L.losa_packed_attn_fwd(q, q[:, :1], q[:, :1], p)
+    with pytest.raises(TypeError, match="PackedPlan"):
+        L.losa_packed_attn_fwd(q, q, q, None)
