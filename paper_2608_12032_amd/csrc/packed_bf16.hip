@@ -136,47 +136,162 @@ __device__ __forceinline__ int wave_min(int x) {
 
 // Per-lane global offsets, inside a sub-tile, of the direct load that fills bytes
 // o .. o + 15 of its LDS image (the images of sparse_fwd.hip, the caller's row strides).
-template <int D, int BLK>
+template <int D>
 __device__ __forceinline__ uint32_t k_offset(int o, uint32_t stride) {
-  using C = FwdCfg<D, BLK, 32>;
+  using C = FwdCfg<D, 32, 32>;
   const int r = o / C::KROW;
-  return r * stride + (kswz<D, BLK, 32>(r, (o % C::KROW) >> 4) << 4);
+  return r * stride + (kswz<D, 32, 32>(r, (o % C::KROW) >> 4) << 4);
 }
-template <int D, int BLK>
+template <int D>
 __device__ __forceinline__ uint32_t v_offset(int o, uint32_t stride) {
-  using C = FwdCfg<D, BLK, 32>;
+  using C = FwdCfg<D, 32, 32>;
   const int rem = o % C::VPC;
   return (4 * (o / C::VPC) + ((rem >> 6) & 3)) * stride + (rem >> 8) * 64 + (rem & 63);
 }
 
-// LDS addresses of a lane's operand reads in K slot 0 (k-step st) and V slot 0.
-template <int D, int BLK>
-__device__ __forceinline__ uint32_t k_operand(uint32_t lds0, int lane, int st) {
-  using C = FwdCfg<D, BLK, 32>;
-  return lds0 + (lane & 31) * C::KROW + (kswz<D, BLK, 32>(lane & 31, 2 * st + (lane >> 5)) << 4);
+// LDS addresses of a lane's operand reads in the K image (k-step st) or V image at `at`.
+template <int D>
+__device__ __forceinline__ uint32_t k_operand(uint32_t at, int lane, int st) {
+  using C = FwdCfg<D, 32, 32>;
+  return at + (lane & 31) * C::KROW + (kswz<D, 32, 32>(lane & 31, 2 * st + (lane >> 5)) << 4);
 }
-template <int D, int BLK>
-__device__ __forceinline__ uint32_t v_operand(uint32_t lds0, int lane) {
-  using C = FwdCfg<D, BLK, 32>;
-  return lds0 + C::RING + (lane >> 5) * C::VPC + ((lane >> 2) & 3) * 64 + ((lane >> 4) & 1) * 32 +
+template <int D>
+__device__ __forceinline__ uint32_t v_operand(uint32_t at, int lane) {
+  using C = FwdCfg<D, 32, 32>;
+  return at + (lane >> 5) * C::VPC + ((lane >> 2) & 3) * 64 + ((lane >> 4) & 1) * 32 +
          (lane & 3) * 8;
 }
 
-// Waves per SIMD the registers are cut for, as in the block-sparse forward; the
-// single waves of few-row units are limited by their rings (64 KiB at d = 128).
-template <int D, int NW>
-constexpr int packed_waves_per_simd() {
-  return NW == 1 ? 1 : (D == 64 ? 4 : 2);
+// Waits of one wave: until at most N of its memory operations are outstanding; until its
+// LDS reads have returned.  Neither lets a memory access move across.
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void lds_reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// One 32-key sub-tile of a unit that is done again because its result was not finite
+// (K and V images at kbase and vbase in LDS): values that are not finite stay out of the
+// matrix products of a sub-tile that some row does not see whole, and are added, key by
+// key, to the rows that see them.  pw: 2 KiB of this wave's for its probabilities.
+template <int D>
+__device__ __forceinline__ void slow_sub(uint32_t kbase, const char* vptr, uint32_t vbase,
+                                         __bf16* pw, const Row<D>& row, int first, int whole,
+                                         float scale_log2, int lane, f32x16_t* oacc, float& m_run,
+                                         float& l_run) {
+  using C = FwdCfg<D, 32, 32>;
+  const int r = lane & 31, g = lane >> 5;
+  f32x16_t cur = {};
+  bf16x8_t pb[2];
+#pragma unroll
+  for (int st = 0; st < C::KS; ++st) {
+    cur = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read16(k_operand<D>(kbase, lane, st)),
+                                                  row.q[st], cur, 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  mask_left(cur, row.left - first, g);
+  const float m_new = fmaxf(m_run, sub_max(cur) * scale_log2);
+  const float alpha = fast_exp2(m_run - m_new);
+  m_run = m_new;
+#pragma unroll
+  for (int db = 0; db < C::DB; ++db) oacc[db] *= alpha;
+  l_run = l_run * alpha + softmax_sub(cur, scale_log2, m_run, pb);
+  const bool all = whole >= first + 32;  // every row sees every key of the sub-tile
+  // (K's image is read: the probabilities may overwrite it)
+  lds_reads_done();
+#pragma unroll
+  for (int st = 0; st < 2; ++st) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      pw[(16 * st + 4 * g + (e & 3) + 8 * (e >> 2)) * 32 + r] = pb[st][e];
+#pragma unroll
+    for (int db = 0; db < C::DB; ++db) {
+      bf16x8_t v = read_v<D, 32, 32>(v_operand<D>(vbase, lane), st, db);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = all || finite((float)v[e]) ? v[e] : (__bf16)0.f;
+      oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[st], oacc[db], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  if (all) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+  for (int key = 0; key < 32; ++key) {
+    const float p = (float)pw[key * 32 + r];
+    const bool sees = first + key < row.left;
+    const char* vrow = vptr + (key >> 2) * C::VPC + (key & 3) * 64 + g * 8;
+#pragma unroll
+    for (int db = 0; db < C::DB; ++db)
+#pragma unroll
+      for (int qd = 0; qd < 4; ++qd) {
+        const bf16x4_t v = *reinterpret_cast<const bf16x4_t*>(vrow + db * 256 + qd * 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (sees && !finite((float)v[e])) oacc[db][4 * qd + e] += p * (float)v[e];
+        __builtin_amdgcn_sched_barrier(0);  // (few registers: nothing here is in a hurry)
+      }
+  }
 }
 
-template <int D, int NW>
-__global__ void __launch_bounds__(64 * NW)
-    __attribute__((amdgpu_waves_per_eu(packed_waves_per_simd<D, NW>())))
+// Whether a result holds a value that is not finite, in a row that counts.
+template <int DB>
+__device__ __forceinline__ bool not_finite(const f32x16_t* oacc, bool counts) {
+  float bad = 0.f;  // becomes NaN
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int t = 0; t < 16; ++t) bad = __builtin_fmaf(oacc[db][t], 0.f, bad);
+  return __ballot(counts && bad != 0.f) != 0;
+}
+
+// Unit of this workgroup: (unit, key head), the heads of a unit side by side.
+__device__ __forceinline__ PackedItem unit_of(const PackedArgs& a, int* kvh) {
+  const int unit = (int)blockIdx.x / a.H_kv;
+  *kvh = (int)blockIdx.x - unit * a.H_kv;
+  return a.items[unit];
+}
+// (A plan's units lie inside q and k; nothing is read or written for one that does not.)
+__device__ __forceinline__ bool inside(const PackedArgs& a, const PackedItem& it) {
+  return it.q0 >= 0 && it.q_len >= 0 && it.q0 + it.q_len <= a.q_rows && it.k0 >= 0 &&
+         it.k_len >= 0 && it.k0 + it.k_len <= a.k_rows && it.c0 >= 0 && it.c1 <= it.k_len &&
+         it.row0 >= 0;
+}
+__device__ __forceinline__ const char* first_key(const void* x, const PackedItem& it, int64_t token,
+                                                 int64_t head, int kvh) {
+  return reinterpret_cast<const char*>(static_cast<const __bf16*>(x) + (it.k0 + it.c0) * token +
+                                       kvh * head);
+}
+
+// Where a row's output goes (elements from o and from lse); at < 0: nowhere.
+struct RowOut {
+  int64_t at, lse;
+};
+__device__ __forceinline__ RowOut row_out(const PackedArgs& a, const PackedItem& it, int kvh, int row) {
+  const int tok = row / a.G;
+  const int64_t head = kvh * a.G + (row - tok * a.G);
+  if (tok >= it.q_len) return {-1, 0};
+  return {(it.q0 + tok) * a.ot + head * a.oh, head * a.lse_head + it.q0 + tok};
+}
+
+// Waves per SIMD the registers are cut for, as in the block-sparse forward.
+template <int D>
+constexpr int packed_waves_per_simd() {
+  return D == 64 ? 4 : 2;
+}
+
+// A tile of 128 rows of one sequence against all its keys: four waves of 32 rows.
+template <int D>
+__global__ void __launch_bounds__(256)
+    __attribute__((amdgpu_waves_per_eu(packed_waves_per_simd<D>())))
     packed_bf16_kernel(const PackedArgs a) {
-  constexpr int BLK = 32 * NW, BK = 32;
+  constexpr int NW = 4, BLK = 32 * NW, BK = 32;
   using C = FwdCfg<D, BLK, BK>;
   constexpr int R = C::R;
   __shared__ __attribute__((aligned(1024))) char smem[2 * C::RING];
+  // where each row's output goes: found with its query, so that the end of the kernel
+  // neither divides nor waits for the plan (11.0 -> 9.3 us a workgroup of 2 sub-tiles)
+  __shared__ RowOut out[BLK];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 
@@ -185,40 +300,27 @@ __global__ void __launch_bounds__(64 * NW)
   for (int db = 0; db < C::DB; ++db) oacc[db] = f32x16_t{};
   float m_run = kNegBig;  // max used for exp2 (log2 units)
   float l_run = 0.f;      // this lane's share of the row sum
+  int hidden;             // keys of the unit that some row does not see, if > 0
   {
     const int lane = threadIdx.x & 63;
     const int g = lane >> 5;
-    const int unit = (int)blockIdx.x / a.H_kv;
-    const int kvh = (int)blockIdx.x - unit * a.H_kv;
-    const PackedItem it = a.items[unit];
-    // (a plan's units lie inside q and k; nothing is read or written for one that does not)
-    if (it.q0 < 0 || it.q_len < 0 || it.q0 + it.q_len > a.q_rows || it.k0 < 0 || it.k_len < 0 ||
-        it.k0 + it.k_len > a.k_rows || it.c0 < 0 || it.c1 > it.k_len || it.row0 < 0)
-      return;
+    int kvh;
+    const PackedItem it = unit_of(a, &kvh);
+    if (!inside(a, it)) return;
     const Extent x = extent<BLK>(it, a.G, a.causal);
     const int n = x.n;
+    hidden = n - x.seen0;
     const int S = ((n + 31) / 32 + 1) & ~1;  // sub-tiles, a multiple of the loop's half
-    const Row<D> row = row_of<D>(a, it, x, kvh, it.row0 + w * 32 + (lane & 31), g);
-    const int left = row.left;
-    const int whole = wave_min(left);
-    const char* kb = reinterpret_cast<const char*>(static_cast<const __bf16*>(a.k) +
-                                                   (it.k0 + it.c0) * a.kt + kvh * a.kh);
-    const char* vb = reinterpret_cast<const char*>(static_cast<const __bf16*>(a.v) +
-                                                   (it.k0 + it.c0) * a.vt + kvh * a.vh);
+    const char* kb = first_key(a.k, it, a.kt, a.kh, kvh);
+    const char* vb = first_key(a.v, it, a.vt, a.vh, kvh);
     const uint32_t ks = (uint32_t)a.kt * 2, vs = (uint32_t)a.vt * 2;
     const float scale_log2 = a.scale_log2;
-    uint32_t ka[C::KS], va = v_operand<D, BLK>(lds0, lane);
-#pragma unroll
-    for (int st = 0; st < C::KS; ++st) ka[st] = k_operand<D, BLK>(lds0, lane, st);
     uint32_t koffs[C::LPW], voffs[C::LPW];
 #pragma unroll
     for (int u = 0; u < C::LPW; ++u) {
-      koffs[u] = k_offset<D, BLK>((w * C::LPW + u) * 1024 + lane * 16, ks);
-      voffs[u] = v_offset<D, BLK>((w * C::LPW + u) * 1024 + lane * 16, vs);
+      koffs[u] = k_offset<D>((w * C::LPW + u) * 1024 + lane * 16, ks);
+      voffs[u] = v_offset<D>((w * C::LPW + u) * 1024 + lane * 16, vs);
     }
-    f32x16_t sc[2];
-    bf16x8_t pb[2][2];
-
     if (S > 0) {
 #pragma unroll
       for (int y = 0; y < R; ++y) {
@@ -232,6 +334,18 @@ __global__ void __launch_bounds__(64 * NW)
             dma16(lds0 + C::RING + y * C::SUB + (w * C::LPW + u) * 1024, vrs, voffs[u], 0);
         }
       }
+    }
+    const Row<D> row = row_of<D>(a, it, x, kvh, it.row0 + w * 32 + (lane & 31), g);
+    if (g == 0) out[w * 32 + lane] = row_out(a, it, kvh, it.row0 + w * 32 + lane);
+    const int left = row.left;
+    const int whole = wave_min(left);
+    uint32_t ka[C::KS], va = v_operand<D>(lds0 + C::RING, lane);
+#pragma unroll
+    for (int st = 0; st < C::KS; ++st) ka[st] = k_operand<D>(lds0, lane, st);
+    f32x16_t sc[2];
+    bf16x8_t pb[2][2];
+
+    if (S > 0) {
       for (int z = (w * 64 + lane) * 16; z < C::SUB; z += 64 * NW * 16)
         *reinterpret_cast<f32x4_t*>(smem + C::RING + (R - 1) * C::SUB + z) = f32x4_t{};
 #pragma unroll
@@ -307,134 +421,55 @@ __global__ void __launch_bounds__(64 * NW)
     }
   }
 
-  const PackedArgs b = late_args();
   const int el = late_lane();
   const int er = el & 31, eg = el >> 5;
-  const int unit = (int)blockIdx.x / b.H_kv;
-  const int kvh = (int)blockIdx.x - unit * b.H_kv;
-  const PackedItem it = b.items[unit];
-  const Extent x = extent<BLK>(it, b.G, b.causal);
-  const int rows = it.q_len * b.G - it.row0 - w * 32;  // rows from this wave's first on
-
-  if (x.seen0 < x.n) {
+  if (hidden > 0) {
     // some row does not see some key of the unit: has a value that is not finite spread?
-    float bad = 0.f;  // becomes NaN
+    const bool mine = not_finite<C::DB>(oacc, out[w * 32 + er].at >= 0);
+    int* const flag = reinterpret_cast<int*>(smem + C::RING);  // (no output passes there)
+    if (el == 0) flag[w] = mine;
+    __syncthreads();
+    bool redo = false;
 #pragma unroll
-    for (int db = 0; db < C::DB; ++db)
-#pragma unroll
-      for (int t = 0; t < 16; ++t) bad = __builtin_fmaf(oacc[db][t], 0.f, bad);
-    bool redo = __ballot(er < rows && bad != 0.f) != 0;
-    if constexpr (NW > 1) {
-      int* const flag = reinterpret_cast<int*>(smem + C::RING);  // (no output passes there)
-      if (el == 0) flag[w] = redo;
-      __syncthreads();
-      redo = false;
-#pragma unroll
-      for (int z = 0; z < NW; ++z) redo = redo || flag[z] != 0;
-    }
+    for (int z = 0; z < NW; ++z) redo = redo || flag[z] != 0;
     if (redo) {
+      const PackedArgs b = late_args();
+      int kvh;
+      const PackedItem it = unit_of(b, &kvh);
+      const Extent x = extent<BLK>(it, b.G, b.causal);
       const Row<D> row = row_of<D>(b, it, x, kvh, it.row0 + w * 32 + er, eg);
-      const int left = row.left, whole = wave_min(left);
-      const char* kb = reinterpret_cast<const char*>(static_cast<const __bf16*>(b.k) +
-                                                     (it.k0 + it.c0) * b.kt + kvh * b.kh);
-      const char* vb = reinterpret_cast<const char*>(static_cast<const __bf16*>(b.v) +
-                                                     (it.k0 + it.c0) * b.vt + kvh * b.vh);
-      const uint32_t va = v_operand<D, BLK>(lds0, el);
+      const int whole = wave_min(row.left);
+      const uint32_t ks = (uint32_t)b.kt * 2, vs = (uint32_t)b.vt * 2;
 #pragma unroll
       for (int db = 0; db < C::DB; ++db) oacc[db] = f32x16_t{};
       m_run = kNegBig;
       l_run = 0.f;
-      // this wave's probabilities of a sub-tile, [key][row], behind K slot 0
       __bf16* const pw = reinterpret_cast<__bf16*>(smem + C::SUB) + w * 32 * 32;
-      static_assert(C::SUB + NW * 2048 <= C::RING, "the probabilities fit the K ring");
+      static_assert(C::SUB + NW * 2048 <= C::RING, "the probabilities fit behind K slot 0");
       for (int s = 0; 32 * s < x.n; ++s) {
-        i32x4_t krs = sub_rsrc<D>(kb, (uint32_t)b.kt * 2, s, x.n);
-        i32x4_t vrs = sub_rsrc<D>(vb, (uint32_t)b.vt * 2, s, x.n);
+        i32x4_t krs = sub_rsrc<D>(first_key(b.k, it, b.kt, b.kh, kvh), ks, s, x.n);
+        i32x4_t vrs = sub_rsrc<D>(first_key(b.v, it, b.vt, b.vh, kvh), vs, s, x.n);
         settle(krs);
         settle(vrs);
         lds_read_barrier();
 #pragma unroll 1
         for (int u = 0; u < C::LPW; ++u) {
           const int o = (w * C::LPW + u) * 1024;
-          dma16(lds0 + o, krs, k_offset<D, BLK>(o + el * 16, (uint32_t)b.kt * 2), 0);
-          dma16(lds0 + C::RING + o, vrs, v_offset<D, BLK>(o + el * 16, (uint32_t)b.vt * 2), 0);
+          dma16(lds0 + o, krs, k_offset<D>(o + el * 16, ks), 0);
+          dma16(lds0 + C::RING + o, vrs, v_offset<D>(o + el * 16, vs), 0);
         }
         wait_vm_barrier<0>();
-        f32x16_t cur = {};
-        bf16x8_t pb[2];
-#pragma unroll
-        for (int st = 0; st < C::KS; ++st) {
-          cur = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              lds_read16(k_operand<D, BLK>(lds0, el, st)), row.q[st], cur, 0, 0, 0);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        mask_left(cur, left - 32 * s, eg);
-        const float m_new = fmaxf(m_run, sub_max(cur) * b.scale_log2);
-        const float alpha = fast_exp2(m_run - m_new);
-        m_run = m_new;
-#pragma unroll
-        for (int db = 0; db < C::DB; ++db) oacc[db] *= alpha;
-        l_run = l_run * alpha + softmax_sub(cur, b.scale_log2, m_run, pb);
-        const bool all = whole >= 32 * (s + 1);  // every row sees every key of the sub-tile
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            pw[(16 * st + 4 * eg + (e & 3) + 8 * (e >> 2)) * 32 + er] = pb[st][e];
-#pragma unroll
-          for (int db = 0; db < C::DB; ++db) {
-            bf16x8_t v = read_v<D, BLK, BK>(va, st, db);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = all || finite((float)v[e]) ? v[e] : (__bf16)0.f;
-            oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[st], oacc[db], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        }
-        if (all) continue;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-        for (int key = 0; key < 32; ++key) {
-          const float p = (float)pw[key * 32 + er];
-          const bool sees = 32 * s + key < left;
-          const char* vrow = smem + C::RING + (key >> 2) * C::VPC + (key & 3) * 64 + eg * 8;
-#pragma unroll
-          for (int db = 0; db < C::DB; ++db)
-#pragma unroll
-            for (int qd = 0; qd < 4; ++qd) {
-              const bf16x4_t v = *reinterpret_cast<const bf16x4_t*>(vrow + db * 256 + qd * 16);
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (sees && !finite((float)v[e])) oacc[db][4 * qd + e] += p * (float)v[e];
-              __builtin_amdgcn_sched_barrier(0);  // (few registers: nothing here is in a hurry)
-            }
-        }
+        slow_sub<D>(lds0, smem + C::RING, lds0 + C::RING, pw, row, 32 * s, whole, b.scale_log2, el,
+                    oacc, m_run, l_run);
       }
       lds_read_barrier();
     }
   }
 
   const float l_tot = add_partner(l_run);
-  if (it.part >= 0) {
-    if (er < rows) {
-      const int64_t at = (int64_t)(it.part + w * 32 + er) * b.H_kv + kvh;
-      float* const po = b.part_o + at * D + 4 * eg;
-#pragma unroll
-      for (int db = 0; db < C::DB; ++db)
-#pragma unroll
-        for (int qd = 0; qd < 4; ++qd) {
-          f32x4_t v;
-#pragma unroll
-          for (int u = 0; u < 4; ++u) v[u] = oacc[db][qd * 4 + u];
-          *reinterpret_cast<f32x4_t*>(po + db * 32 + qd * 8) = v;
-        }
-      if (eg == 0) *reinterpret_cast<f32x2_t*>(b.part_ml + 2 * at) = f32x2_t{m_run, l_tot};
-    }
-    return;
-  }
+  const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
   // O leaves through this wave's part of the K ring, which no wave reads any more, so
   // that a store instruction writes whole rows
-  const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
   char* const ot = smem + w * 32 * C::KROW;
 #pragma unroll
   for (int db = 0; db < C::DB; ++db)
@@ -449,27 +484,187 @@ __global__ void __launch_bounds__(64 * NW)
     }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
+  const PackedArgs b = late_args();
 #pragma unroll
   for (int z = 0; z < C::SUB; z += 1024) {
     const int r = (z + el * 16) / C::KROW, c = (el * 16 % C::KROW) >> 4;
-    if (r >= rows) continue;
-    const int gr = it.row0 + w * 32 + r, t = gr / b.G;
-    __bf16* const op = static_cast<__bf16*>(b.o) + (it.q0 + t) * b.ot +
-                       (int64_t)(kvh * b.G + (gr - t * b.G)) * b.oh;
-    *reinterpret_cast<f32x4_t*>(op + 8 * c) =
-        *reinterpret_cast<const f32x4_t*>(ot + r * C::KROW + (kswz<D, BLK, BK>(r, c) << 4));
+    const int64_t at = out[w * 32 + r].at;
+    if (at >= 0)
+      *reinterpret_cast<f32x4_t*>(static_cast<__bf16*>(b.o) + at + 8 * c) =
+          *reinterpret_cast<const f32x4_t*>(ot + r * C::KROW + (kswz<D, BLK, BK>(r, c) << 4));
   }
-  if (b.lse != nullptr && eg == 0 && er < rows) {
-    const int gr = it.row0 + w * 32 + er, t = gr / b.G;
-    b.lse[(int64_t)(kvh * b.G + (gr - t * b.G)) * b.lse_head + it.q0 + t] =
-        l_tot == 0.f ? -INFINITY : (m_run + __log2f(l_tot)) * kLn2;
+  if (b.lse != nullptr && eg == 0 && out[w * 32 + er].at >= 0)
+    b.lse[out[w * 32 + er].lse] = l_tot == 0.f ? -INFINITY : (m_run + __log2f(l_tot)) * kLn2;
+}
+
+// A part of the keys of a sequence of few rows: its rows fit one 32-row tile, and four
+// waves take the part's sub-tiles in turn, each through one K and one V slot of its own,
+// so that the loop has no barrier: K's slot is refilled while the softmax runs, V's while
+// the next scores do.  The waves' states are merged in LDS in wave order.
+//
+// Bound: HBM.  Two workgroups a CU (d = 128) keep 128 KiB in flight there.
+template <int D>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+    few_bf16_kernel(const PackedArgs a) {
+  constexpr int NW = 4;
+  using C = FwdCfg<D, 32, 32>;
+  constexpr int LD = C::LPW;  // loads of a sub-tile
+  __shared__ __attribute__((aligned(1024))) char smem[NW * 2 * C::SUB];
+  __shared__ float ml[NW][32][2];
+  __shared__ RowOut out[32];
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int r32 = lane & 31, g = lane >> 5;
+  const uint32_t lds0 =
+      (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + w * 2 * C::SUB;
+  char* const vptr = smem + w * 2 * C::SUB + C::SUB;
+  int kvh;
+  const PackedItem it = unit_of(a, &kvh);
+  if (!inside(a, it)) return;
+  const Extent x = extent<32>(it, a.G, a.causal);
+  const int n = x.n;
+  const char* kb = first_key(a.k, it, a.kt, a.kh, kvh);
+  const char* vb = first_key(a.v, it, a.vt, a.vh, kvh);
+  const uint32_t ks = (uint32_t)a.kt * 2, vs = (uint32_t)a.vt * 2;
+  uint32_t koffs[LD], voffs[LD];
+#pragma unroll
+  for (int u = 0; u < LD; ++u) {
+    koffs[u] = k_offset<D>(u * 1024 + lane * 16, ks);
+    voffs[u] = v_offset<D>(u * 1024 + lane * 16, vs);
+  }
+  auto load_k = [&](int s) {
+    i32x4_t rs = sub_rsrc<D>(kb, ks, s, n);
+    settle(rs);
+#pragma unroll
+    for (int u = 0; u < LD; ++u) dma16(lds0 + u * 1024, rs, koffs[u], 0);
+  };
+  auto load_v = [&](int s) {
+    i32x4_t rs = sub_rsrc<D>(vb, vs, s, n);
+    settle(rs);
+#pragma unroll
+    for (int u = 0; u < LD; ++u) dma16(lds0 + C::SUB + u * 1024, rs, voffs[u], 0);
+  };
+  if (32 * w < n) {
+    load_k(w);
+    load_v(w);
+  }
+  Row<D> row = row_of<D>(a, it, x, kvh, it.row0 + r32, g);
+  // (waited for here, not inside the loop, where the wait would cover the loads in flight)
+#pragma unroll
+  for (int st = 0; st < C::KS; ++st) asm volatile("" : "+v"(row.q[st]));
+  if (w == 0 && g == 0) out[lane] = row_out(a, it, kvh, it.row0 + lane);
+  const int whole = wave_min(row.left);
+  f32x16_t oacc[C::DB];
+#pragma unroll
+  for (int db = 0; db < C::DB; ++db) oacc[db] = f32x16_t{};
+  float m_run = kNegBig, l_run = 0.f;
+  for (int s = w; 32 * s < n; s += NW) {
+    wait_vm<LD>();  // K is there (V's loads are the last)
+    f32x16_t cur = {};
+#pragma unroll
+    for (int st = 0; st < C::KS; ++st)
+      cur = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read16(k_operand<D>(lds0, lane, st)),
+                                                    row.q[st], cur, 0, 0, 0);
+    lds_reads_done();
+    load_k(s + NW);  // (behind the end: zeros)
+    if (whole < 32 * (s + 1)) mask_left(cur, row.left - 32 * s, g);
+    const float m_new = fmaxf(m_run, sub_max(cur) * a.scale_log2);
+    if (__ballot(m_new > m_run) != 0) {
+      const float alpha = fast_exp2(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < C::DB; ++db) oacc[db] *= alpha;
+    }
+    bf16x8_t pb[2];
+    l_run += softmax_sub(cur, a.scale_log2, m_run, pb);
+    wait_vm<LD>();  // V is there
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int db = 0; db < C::DB; ++db)
+        oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            read_v<D, 32, 32>(v_operand<D>(lds0 + C::SUB, lane), st, db), pb[st], oacc[db], 0, 0, 0);
+    lds_reads_done();
+    load_v(s + NW);
+  }
+  wait_vm<0>();
+  if (n > x.seen0 && not_finite<C::DB>(oacc, r32 < it.q_len * a.G - it.row0)) {
+    // some row does not see some key: this wave's sub-tiles again, see slow_sub
+#pragma unroll
+    for (int db = 0; db < C::DB; ++db) oacc[db] = f32x16_t{};
+    m_run = kNegBig;
+    l_run = 0.f;
+    for (int s = w; 32 * s < n; s += NW) {
+      lds_reads_done();
+      load_k(s);
+      load_v(s);
+      wait_vm<0>();
+      slow_sub<D>(lds0, vptr, lds0 + C::SUB, reinterpret_cast<__bf16*>(vptr - C::SUB), row, 32 * s,
+                  whole, a.scale_log2, lane, oacc, m_run, l_run);
+    }
+    lds_reads_done();
+  }
+
+  // the waves' states through LDS: O of wave w, [row][d] in 16-byte chunks swizzled by
+  // row, over its own slots
+  const float l_tot = add_partner(l_run);
+  const int rows = it.q_len * a.G - it.row0;
+  constexpr int CH = D / 4;  // chunks of a row
+  auto chunk = [&](int wave, int r, int c) {
+    return reinterpret_cast<f32x4_t*>(smem + wave * 2 * C::SUB + (r * CH + (c ^ (r % CH))) * 16);
+  };
+  if (r32 < rows) {
+#pragma unroll
+    for (int db = 0; db < C::DB; ++db)
+#pragma unroll
+      for (int qd = 0; qd < 4; ++qd) {
+        f32x4_t v;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = oacc[db][qd * 4 + u];
+        *chunk(w, r32, db * 8 + qd * 2 + g) = v;
+      }
+    if (g == 0) {
+      ml[w][r32][0] = m_run;
+      ml[w][r32][1] = l_tot;
+    }
+  }
+  __syncthreads();
+  const int used = rows < 32 ? rows : 32;
+  for (int i = threadIdx.x; i < used * CH; i += 64 * NW) {
+    const int r = i / CH, c = i % CH;
+    float m = kNegBig, l = 0.f;
+#pragma unroll
+    for (int y = 0; y < NW; ++y) m = fmaxf(m, ml[y][r][0]);
+    f32x4_t acc = {};
+#pragma unroll
+    for (int y = 0; y < NW; ++y) {
+      const float f = fast_exp2(ml[y][r][0] - m);
+      l = __builtin_fmaf(ml[y][r][1], f, l);
+      const f32x4_t v = *chunk(y, r, c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(v[e], f, acc[e]);
+    }
+    if (it.part >= 0) {
+      const int64_t at = (int64_t)(it.part + r) * a.H_kv + kvh;
+      *reinterpret_cast<f32x4_t*>(a.part_o + at * D + 4 * c) = acc;
+      if (c == 0) *reinterpret_cast<f32x2_t*>(a.part_ml + 2 * at) = f32x2_t{m, l};
+    } else if (out[r].at >= 0) {
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] *= inv;
+      *reinterpret_cast<bf16x4_t*>(static_cast<__bf16*>(a.o) + out[r].at + 4 * c) =
+          __builtin_convertvector(acc, bf16x4_t);
+      if (a.lse != nullptr && c == 0)
+        a.lse[out[r].lse] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
+    }
   }
 }
 
 // Rows whose keys were split: one workgroup per row and key head takes the parts'
-// common max, then their sums and outputs rescaled to it, each wave every fourth
+// common max, then their sums and outputs rescaled to it, each wave every eighth
 // part, the waves added in order.
-constexpr int kJoinWaves = 4;
+constexpr int kJoinWaves = 8;
 
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(const PackedArgs a) {
@@ -491,7 +686,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(const PackedArgs 
 #pragma unroll
   for (int x = 0; x < kJoinWaves; ++x) m = fmaxf(m, red[x]);
   float l = 0.f, acc[PL] = {};
-#pragma unroll 4
+#pragma unroll 8
   for (int i = w; i < j.n; i += kJoinWaves) {
     const f32x2_t ml = *reinterpret_cast<const f32x2_t*>(a.part_ml + 2 * at(i));
     const float* po = a.part_o + at(i) * D + lane * PL;
@@ -522,13 +717,13 @@ __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(const PackedArgs 
 template <int D>
 hipError_t launch(const PackedArgs& a, int n_tiles, int n_few, hipStream_t stream) {
   if (n_tiles > 0)
-    hipLaunchKernelGGL((packed_bf16_kernel<D, 4>), dim3((uint32_t)n_tiles * a.H_kv), dim3(256), 0,
+    hipLaunchKernelGGL((packed_bf16_kernel<D>), dim3((uint32_t)n_tiles * a.H_kv), dim3(256), 0,
                        stream, a);
   if (n_few > 0) {
     PackedArgs few = a;
     few.items += n_tiles;
-    hipLaunchKernelGGL((packed_bf16_kernel<D, 1>), dim3((uint32_t)n_few * a.H_kv), dim3(64), 0,
-                       stream, few);
+    hipLaunchKernelGGL((few_bf16_kernel<D>), dim3((uint32_t)n_few * a.H_kv), dim3(256), 0, stream,
+                       few);
   }
   return hipGetLastError();
 }

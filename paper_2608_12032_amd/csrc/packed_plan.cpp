@@ -10,12 +10,12 @@ namespace losa {
 
 namespace {
 
-// Keys of a part of a few-row sequence (a multiple of the 32-key sub-tile).
-// bf16: a part is one wave.  128 keys at least, so that a part's partial rows stay
-// small beside its K and V; 256 parts at most, so that the join stays short.  fp32: a
-// part is a workgroup of eight waves, two sub-tiles each at least.
+// Keys of a part of a few-row sequence (a multiple of the 32-key sub-tile): one
+// workgroup of four waves (bf16) or eight (fp32), two sub-tiles each at least, so that a
+// part's partial rows stay small beside its K and V; 256 parts at most, so that the
+// join stays short.
 int part_keys(bool bf16, int k_len) {
-  const int least = bf16 ? 128 : 512;
+  const int least = bf16 ? 256 : 512;
   const int64_t even = ((int64_t)k_len + 255) / 256;
   const int64_t keys = (even + 63) / 64 * 64;
   return (int)(keys < least ? least : keys);

@@ -429,6 +429,9 @@ class RopeTable:
 
     def __init__(self, data, axis_dim, axis_len):
         self.data, self.axis_dim, self.axis_len = data, tuple(axis_dim), tuple(axis_len)
+        n, ints = len(self.axis_dim), ctypes.c_int * MAX_AXES
+        self._form = _Rotation(n, ints(*self.axis_dim), ints(*self.axis_len))
+        self._floats = sum(a * b for a, b in zip(self.axis_dim, self.axis_len))
 
 
 def losa_rope_table(axis_dim, axis_len, base: float = 10000.0, device="cuda") -> RopeTable:
@@ -448,22 +451,25 @@ def losa_rope_table(axis_dim, axis_len, base: float = 10000.0, device="cuda") ->
     return RopeTable(host.to(device), axis_dim, axis_len)
 
 
-def _view(t, name, device, dtype, shape):
-    """losa_view of a [B, N, H, d] tensor whose rows of d are contiguous."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    if not t.is_cuda or t.device != device:
-        raise ValueError(f"{name} must live on {device} (got {t.device})")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
-    if tuple(t.shape) != tuple(shape):
+def _view(t, name, device, dtype, shape, swap=False):
+    """losa_view of a [B, N, H, d] tensor (swap: [B, H, N, d]) of this shape, whose rows
+    of d are contiguous."""
+    if not (isinstance(t, torch.Tensor) and t.device == device and t.is_cuda and t.dtype == dtype
+            and t.shape == shape):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if not t.is_cuda or t.device != device:
+            raise ValueError(f"{name} must live on {device} (got {t.device})")
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
         raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
     sb, sn, sh, sd = t.stride()
     if sd != 1:
         raise ValueError(f"{name} must have contiguous rows (stride 1 in the last dim)")
     # (a stride along one element is never used, and torch may set it to anything)
-    B, N, H, _ = t.shape
-    return _View(t.data_ptr(), sb if B > 1 else 0, sn if N > 1 else 0, sh if H > 1 else 0)
+    B, N, H, _ = shape
+    sb, sn, sh = sb if B > 1 else 0, sn if N > 1 else 0, sh if H > 1 else 0
+    return _View(t.data_ptr(), sb, sh, sn) if swap else _View(t.data_ptr(), sb, sn, sh)
 
 
 def _rotation(table, pos, pairing, B, N, device):
@@ -471,16 +477,17 @@ def _rotation(table, pos, pairing, B, N, device):
     if not isinstance(table, RopeTable):
         raise TypeError("table must be a RopeTable (losa_rope_table)")
     n = len(table.axis_dim)
-    _arg(table.data, "table", device, dtype=torch.float32,
-         numel=sum(a * b for a, b in zip(table.axis_dim, table.axis_len)))
+    _arg(table.data, "table", device, dtype=torch.float32, numel=table._floats)
     _arg(pos, "pos", device, dtype=torch.int32)
-    if tuple(pos.shape) not in ((n, N), (B, n, N)):
+    if pos.shape != (n, N) and pos.shape != (B, n, N):
         raise ValueError(f"pos must have shape {(n, N)} or {(B, n, N)} (got {tuple(pos.shape)})")
     if pairing not in PAIRS:
         raise ValueError(f"pairing must be one of {tuple(PAIRS)} (got {pairing!r})")
-    ints = ctypes.c_int * MAX_AXES
-    return _Rotation(n, ints(*table.axis_dim), ints(*table.axis_len), table.data.data_ptr(),
-                     pos.data_ptr(), n * N if pos.dim() == 3 else 0, PAIRS[pairing])
+    rot = _Rotation.from_buffer_copy(table._form)
+    rot.table, rot.pos, rot.pairs = table.data.data_ptr(), pos.data_ptr(), PAIRS[pairing]
+    if pos.dim() == 3:
+        rot.pos_batch = n * N
+    return rot
 
 
 def _rows_in(t, name):
@@ -490,13 +497,21 @@ def _rows_in(t, name):
 
 
 def _rows_out(out, name, x, n_pad):
-    """The output [B, H, n_pad, d] for x [B, N, H, d], as a view of [B, n_pad, H, d]."""
+    """The output [B, H, n_pad, d] for x [B, N, H, d], and its losa_view."""
     B, _, H, d = x.shape
     if out is None:
         out = torch.empty((B, H, n_pad, d), dtype=x.dtype, device=x.device)
-    if not isinstance(out, torch.Tensor) or out.dim() != 4:
+    elif not isinstance(out, torch.Tensor) or out.dim() != 4:
         raise ValueError(f"{name} must be a [B, H, n_pad, d] tensor")
-    return out, _view(out.transpose(1, 2), name, x.device, x.dtype, (B, n_pad, H, d))
+    return out, _view(out, name, x.device, x.dtype, (B, H, n_pad, d), swap=True)
+
+
+def _call(device, fn, *args):
+    """fn(*args, stream) on the device's current stream, with that device current."""
+    if torch.cuda.current_device() == device.index:
+        return fn(*args, _stream(device))
+    with torch.cuda.device(device):
+        return fn(*args, _stream(device))
 
 
 def losa_rope(x, table: RopeTable, pos, n_pad: int | None = None, pairing: str = "interleaved",
@@ -506,14 +521,12 @@ def losa_rope(x, table: RopeTable, pos, n_pad: int | None = None, pairing: str =
     ``out`` may have any strides, and may be x's own memory."""
     B, N, H, d = _rows_in(x, "x")
     n_pad = N if n_pad is None else n_pad
-    dcode = _dtype_code(x)
-    xv = _view(x, "x", x.device, x.dtype, x.shape)
-    rot = _rotation(table, pos, pairing, B, N, x.device)
+    dev, dcode, at = x.device, _dtype_code(x), ctypes.addressof
+    xv = _view(x, "x", dev, x.dtype, x.shape)
+    rot = _rotation(table, pos, pairing, B, N, dev)
     out, yv = _rows_out(out, "out", x, n_pad)
-    with torch.cuda.device(x.device):
-        st = lib.losa_rope(ctypes.addressof(xv), dcode, B, N, n_pad, H, d, ctypes.addressof(rot),
-                           ctypes.addressof(yv), _stream(x.device))
-    _check(st, "losa_rope")
+    _check(_call(dev, lib.losa_rope, at(xv), dcode, B, N, n_pad, H, d, at(rot), at(yv)),
+           "losa_rope")
     return out
 
 
@@ -527,24 +540,25 @@ def losa_qk_norm_rope(q, k, v=None, *, norm: str | None = "rms", over: str = "he
     strides; weights and biases fp32 of d or heads * d elements."""
     B, N, H, d = _rows_in(q, "q")
     Hkv = _rows_in(k, "k")[2]
-    dev = q.device
+    dev, dt, at = q.device, q.dtype, ctypes.addressof
     n_pad = N if n_pad is None else n_pad
     dcode = _dtype_code(q)
     if over not in ("head", "all"):
         raise ValueError(f"over must be 'head' or 'all' (got {over!r})")
-    views = [_view(q, "q", dev, q.dtype, q.shape), _view(k, "k", dev, q.dtype, (B, N, Hkv, d)),
-             None if v is None else _view(v, "v", dev, q.dtype, (B, N, Hkv, d))]
+    qi, ki = _view(q, "q", dev, dt, q.shape), _view(k, "k", dev, dt, (B, N, Hkv, d))
+    vi = None if v is None else _view(v, "v", dev, dt, (B, N, Hkv, d))
     args = None
     if norm is not None:
         if norm not in NORMS:
             raise ValueError(f"norm must be None or one of {tuple(NORMS)} (got {norm!r})")
-        for name, t, heads in (("q_weight", q_weight, H), ("q_bias", q_bias, H),
-                               ("k_weight", k_weight, Hkv), ("k_bias", k_bias, Hkv)):
+        all_heads = over == "all"
+        span, span_kv = (H * d, Hkv * d) if all_heads else (d, d)
+        for name, t, n in (("q_weight", q_weight, span), ("q_bias", q_bias, span),
+                           ("k_weight", k_weight, span_kv), ("k_bias", k_bias, span_kv)):
             if t is not None:
-                _arg(t, name, dev, dtype=torch.float32,
-                     shape=(d if over == "head" else heads * d,))
-        args = _QkNorm(NORMS[norm], over == "all", eps, _ptr(q_weight), _ptr(q_bias),
-                       _ptr(k_weight), _ptr(k_bias))
+                _arg(t, name, dev, dtype=torch.float32, shape=(n,))
+        args = _QkNorm(NORMS[norm], all_heads, eps, _ptr(q_weight), _ptr(q_bias), _ptr(k_weight),
+                       _ptr(k_bias))
     elif not (q_weight is q_bias is k_weight is k_bias is None):
         raise ValueError("weights and biases need a norm")
     if (table is None) != (pos is None):
@@ -552,16 +566,12 @@ def losa_qk_norm_rope(q, k, v=None, *, norm: str | None = "rms", over: str = "he
     rot = None if table is None else _rotation(table, pos, pairing, B, N, dev)
     if v is None and v_out is not None:
         raise ValueError("v_out needs v")
-    q_out, qv = _rows_out(q_out, "q_out", q, n_pad)
-    k_out, kv = _rows_out(k_out, "k_out", k, n_pad)
-    vv = None
+    q_out, qo = _rows_out(q_out, "q_out", q, n_pad)
+    k_out, ko = _rows_out(k_out, "k_out", k, n_pad)
     if v is not None:
-        v_out, vv = _rows_out(v_out, "v_out", v, n_pad)
-    at = lambda x: None if x is None else ctypes.addressof(x)  # noqa: E731
-    with torch.cuda.device(dev):
-        st = lib.losa_qk_norm_rope(at(views[0]), at(views[1]), at(views[2]), dcode, B, N, n_pad, H,
-                                   Hkv, d, at(args), at(rot), at(qv), at(kv), at(vv),
-                                   _stream(dev))
+        v_out, vo = _rows_out(v_out, "v_out", v, n_pad)
+    st = _call(dev, lib.losa_qk_norm_rope, at(qi), at(ki), vi and at(vi), dcode, B, N, n_pad, H,
+               Hkv, d, args and at(args), rot and at(rot), at(qo), at(ko), vi and at(vo))
     _check(st, "losa_qk_norm_rope")
     return (q_out, k_out) if v is None else (q_out, k_out, v_out)
 
@@ -575,9 +585,10 @@ class PackedPlan:
         self.q_rows, self.k_rows = info.q_rows, info.k_rows
         self.heads, self.kv_heads = info.H, info.H_kv
         self._at = ctypes.addressof(info)
+        self._need = {d: int(lib.losa_packed_workspace_bytes(self._at, d)) for d in (64, 128)}
 
     def workspace_bytes(self, d: int) -> int:
-        return int(lib.losa_packed_workspace_bytes(self._at, d))
+        return self._need.get(d, 0)
 
     def workspace(self, d: int):
         """A workspace for losa_packed_attn_fwd at head dim d, None where it needs none."""
@@ -619,11 +630,24 @@ def losa_packed_plan(q_lens, k_lens, heads: int, kv_heads: int, dtype, causal: b
     return PackedPlan(info, host.to(device), dtype)
 
 
-def _packed_view(t, name, device, dtype, heads, d):
-    """losa_view of a [rows, heads, d] tensor whose rows of d are contiguous."""
+def _packed_view(t, name, device, dtype, rows, heads, d):
+    """losa_view of a [rows, heads, d] tensor (rows None: any number of them) whose rows
+    of d are contiguous."""
     if not isinstance(t, torch.Tensor) or t.dim() != 3:
         raise ValueError(f"{name} must be a [rows, heads, d] tensor")
-    return _view(t[None], name, device, dtype, (1, t.shape[0], heads, d))
+    shape = t.shape
+    if not (t.device == device and t.is_cuda and t.dtype == dtype and shape[1] == heads
+            and shape[2] == d and (rows is None or shape[0] == rows)):
+        if not t.is_cuda or t.device != device:
+            raise ValueError(f"{name} must live on {device} (got {t.device})")
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
+        raise ValueError(f"{name} must have shape {('any' if rows is None else rows, heads, d)} "
+                         f"(got {tuple(shape)})")
+    sn, sh, sd = t.stride()
+    if sd != 1:
+        raise ValueError(f"{name} must have contiguous rows (stride 1 in the last dim)")
+    return _View(t.data_ptr(), 0, sn if shape[0] > 1 else 0, sh if heads > 1 else 0)
 
 
 def losa_packed_attn_fwd(q, k, v, plan: PackedPlan, scale: float | None = None,
@@ -635,37 +659,32 @@ def losa_packed_attn_fwd(q, k, v, plan: PackedPlan, scale: float | None = None,
         raise TypeError("plan must be a PackedPlan (losa_packed_plan)")
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a [rows, heads, d] tensor")
-    dev, d = q.device, q.shape[2]
+    rows, _, d = q.shape
+    dev, dt, at = q.device, plan.dtype, ctypes.addressof
     if plan.data.device != dev:
-        raise ValueError(f"the plan must live on {dev} (got {plan.data.device})")
-    rows = q.shape[0]
-    qv = _packed_view(q, "q", dev, plan.dtype, plan.heads, d)
-    kv = _packed_view(k, "k", dev, plan.dtype, plan.kv_heads, d)
-    vv = _packed_view(v, "v", dev, plan.dtype, plan.kv_heads, d)
-    if k.shape[0] != v.shape[0]:
-        raise ValueError(f"k has {k.shape[0]} rows, v {v.shape[0]}")
+        raise ValueError(f"q and the plan must live on one device (got {dev}, {plan.data.device})")
+    qv = _packed_view(q, "q", dev, dt, None, plan.heads, d)
+    kv = _packed_view(k, "k", dev, dt, None, plan.kv_heads, d)
+    vv = _packed_view(v, "v", dev, dt, None, plan.kv_heads, d)
+    k_rows = k.shape[0]
+    if k_rows != v.shape[0]:
+        raise ValueError(f"k has {k_rows} rows, v {v.shape[0]}")
     if out is None:
-        out = torch.empty((rows, plan.heads, d), dtype=q.dtype, device=dev)
-    ov = _packed_view(out, "out", dev, plan.dtype, plan.heads, d)
-    if out.shape[0] != rows:
-        raise ValueError(f"out must have shape {tuple(q.shape)} (got {tuple(out.shape)})")
-    if want_lse and lse is None:
-        lse = torch.empty((plan.heads, rows), dtype=torch.float32, device=dev)
+        out = torch.empty((rows, plan.heads, d), dtype=dt, device=dev)
+    ov = _packed_view(out, "out", dev, dt, rows, plan.heads, d)
     if want_lse:
+        if lse is None:
+            lse = torch.empty((plan.heads, rows), dtype=torch.float32, device=dev)
         _arg(lse, "lse", dev, dtype=torch.float32, shape=(plan.heads, rows))
     need = plan.workspace_bytes(d)
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    ws_bytes = 0
     if workspace is not None:
-        _arg(workspace, "workspace", dev, nbytes=need)
-    ws_bytes = 0 if workspace is None else workspace.nbytes
-    scale = 1.0 / math.sqrt(d) if scale is None else scale
-    at = ctypes.addressof
-    with torch.cuda.device(dev):
-        st = lib.losa_packed_attn_fwd(at(qv), at(kv), at(vv), rows, k.shape[0], plan._at,
-                                      plan.data.data_ptr(), d, scale, at(ov),
-                                      _ptr(lse if want_lse else None), rows, _ptr(workspace),
-                                      ws_bytes, _stream(dev))
+        ws_bytes = _arg(workspace, "workspace", dev, nbytes=need).nbytes
+    st = _call(dev, lib.losa_packed_attn_fwd, at(qv), at(kv), at(vv), rows, k_rows, plan._at,
+               plan.data.data_ptr(), d, 1.0 / math.sqrt(d) if scale is None else scale, at(ov),
+               _ptr(lse if want_lse else None), rows, _ptr(workspace), ws_bytes)
     _check(st, "losa_packed_attn_fwd")
     return (out, lse) if want_lse else out
 
