@@ -392,6 +392,7 @@ typedef struct {
   int64_t q_rows, k_rows; /* rows that q and o, and k and v, must have                     */
   int64_t part_rows;      /* rows of partial results (the workspace's size)                */
   int32_t n_tiles, n_few, n_joins; /* units of work                                        */
+  int32_t tile_rows;
   int32_t H, H_kv, causal;
   losa_dtype dtype;
 } losa_packed_info;

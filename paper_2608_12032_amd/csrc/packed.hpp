@@ -34,11 +34,15 @@ struct PackedArgs {
   int64_t lse_head;
   int64_t q_rows, k_rows;
   int H_kv, G, causal;
+  int n_tiles;  // items below this are tiles, the others parts of few-row sequences
+  int tile_rows;
   float scale_log2;
 };
-// Rows of a tile, rows of a sequence that make it a few-row one, keys of a part.
+// Rows of a tile (fp32: of a wide one; a call of few units takes tiles of 16), rows of
+// a sequence that make it a few-row one.
 constexpr int kPackedTile[2] = {32, 128};  // [bf16]
 constexpr int kPackedFew[2] = {16, 32};
+constexpr int kPackedNarrow = 16;
 // The sequences of a call as the plan takes them (starts null: one after another).
 struct PackedSeqs {
   const int64_t *q_start, *k_start;
@@ -48,6 +52,7 @@ struct PackedSeqs {
 };
 struct PackedCounts {
   int tiles, few, joins;
+  int tile_rows;
   int64_t part_rows;
 };
 // False: more units than a launch takes.  The plan is tiles, few-row units, joins.
@@ -56,8 +61,8 @@ void packed_fill(const PackedSeqs& s, const PackedCounts& n, void* plan);
 inline size_t packed_plan_bytes(const PackedCounts& n) {
   return ((size_t)n.tiles + n.few) * sizeof(PackedItem) + (size_t)n.joins * sizeof(PackedJoin);
 }
-hipError_t launch_packed_bf16(int d, const PackedArgs& a, int n_tiles, int n_few, hipStream_t stream);
-hipError_t launch_packed_f32(int d, const PackedArgs& a, int n_tiles, int n_few, hipStream_t stream);
+hipError_t launch_packed_bf16(int d, const PackedArgs& a, int n_few, hipStream_t stream);
+hipError_t launch_packed_f32(int d, const PackedArgs& a, int n_few, hipStream_t stream);
 hipError_t launch_packed_join(int d, bool bf16, const PackedArgs& a, int n_joins, hipStream_t stream);
 
 }  // namespace losa

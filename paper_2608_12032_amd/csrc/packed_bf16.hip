@@ -274,24 +274,29 @@ __device__ __forceinline__ RowOut row_out(const PackedArgs& a, const PackedItem&
   return {(it.q0 + tok) * a.ot + head * a.oh, head * a.lse_head + it.q0 + tok};
 }
 
-// Waves per SIMD the registers are cut for, as in the block-sparse forward.
+constexpr int NW = 4;  // waves of a workgroup
+
+// LDS of a workgroup.
 template <int D>
-constexpr int packed_waves_per_simd() {
-  return D == 64 ? 4 : 2;
-}
+struct PackedLds {
+  // tile: the rings; few rows: each wave's K and V slot, then its O
+  static constexpr int BYTES = 2 * FwdCfg<D, 32 * NW, 32>::RING;
+  static_assert(BYTES == NW * 2 * FwdCfg<D, 32, 32>::SUB, "one size for both");
+  __attribute__((aligned(1024))) char smem[BYTES];
+  // where each row's output goes: found with its query, so that the end of the kernel
+  // neither divides nor waits for the plan
+  RowOut out[32 * NW];
+  float ml[NW][32][2];
+};
 
 // A tile of 128 rows of one sequence against all its keys: four waves of 32 rows.
 template <int D>
-__global__ void __launch_bounds__(256)
-    __attribute__((amdgpu_waves_per_eu(packed_waves_per_simd<D>())))
-    packed_bf16_kernel(const PackedArgs a) {
-  constexpr int NW = 4, BLK = 32 * NW, BK = 32;
+__device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds) {
+  constexpr int BLK = 32 * NW, BK = 32;
   using C = FwdCfg<D, BLK, BK>;
   constexpr int R = C::R;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * C::RING];
-  // where each row's output goes: found with its query, so that the end of the kernel
-  // neither divides nor waits for the plan (11.0 -> 9.3 us a workgroup of 2 sub-tiles)
-  __shared__ RowOut out[BLK];
+  char* const smem = lds.smem;
+  RowOut* const out = lds.out;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 
@@ -504,14 +509,12 @@ __global__ void __launch_bounds__(256)
 //
 // Bound: HBM.  Two workgroups a CU (d = 128) keep 128 KiB in flight there.
 template <int D>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
-    few_bf16_kernel(const PackedArgs a) {
-  constexpr int NW = 4;
+__device__ __forceinline__ void few_unit(const PackedArgs& a, PackedLds<D>& lds) {
   using C = FwdCfg<D, 32, 32>;
   constexpr int LD = C::LPW;  // loads of a sub-tile
-  __shared__ __attribute__((aligned(1024))) char smem[NW * 2 * C::SUB];
-  __shared__ float ml[NW][32][2];
-  __shared__ RowOut out[32];
+  char* const smem = lds.smem;
+  RowOut* const out = lds.out;
+  auto& ml = lds.ml;
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int r32 = lane & 31, g = lane >> 5;
@@ -661,79 +664,129 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
   }
 }
 
-// Rows whose keys were split: one workgroup per row and key head takes the parts'
-// common max, then their sums and outputs rescaled to it, each wave every eighth
-// part, the waves added in order.
+// Waves per SIMD the registers are cut for, as in the block-sparse forward.
+template <int D>
+constexpr int packed_waves_per_simd() {
+  return D == 64 ? 4 : 2;
+}
+
+// Tiles come first in a plan, then few-row parts.  At d = 128 one kernel runs both (10
+// prompts of 1 to 1,024 tokens: 33.8 us, in two launches 39.8).  At d = 64 the tiles' 128
+// registers leave no room for that (142 us alone, 200 in one kernel: it spills).
+constexpr int kTiles = 1, kFew = 2;
+template <int D, int KINDS>
+__global__ void __launch_bounds__(64 * NW)
+    __attribute__((amdgpu_waves_per_eu(KINDS == kFew ? 2 : packed_waves_per_simd<D>())))
+    packed_bf16_kernel(const PackedArgs a) {
+  __shared__ PackedLds<D> lds;
+  if (KINDS == kTiles || (KINDS != kFew && (int)blockIdx.x < a.n_tiles * a.H_kv))
+    tile_unit<D>(a, lds);
+  else
+    few_unit<D>(a, lds);
+}
+
+// Rows whose keys were split: one workgroup per row and key head.  Wave w takes parts w,
+// w + 8, ... (lane t the max and sum of its t-th), rescales their outputs to the wave's
+// max and adds them in order; the waves' states are then merged in order.  The outputs'
+// loads do not wait for the weights.
 constexpr int kJoinWaves = 8;
+constexpr int kJoinMost = 32;  // parts of a wave: a plan has 256 at most
 
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(const PackedArgs a) {
   constexpr int PL = D / 64;  // values per lane
-  __shared__ float red[kJoinWaves];
-  __shared__ float lpart[kJoinWaves];
+  __shared__ float ml[kJoinWaves][2];
   __shared__ float opart[kJoinWaves][D];
   const int unit = (int)blockIdx.x / a.H_kv;
   const int kvh = (int)blockIdx.x - unit * a.H_kv;
   const PackedJoin j = a.joins[unit];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   auto at = [&](int i) { return (int64_t)(j.part + (int64_t)i * j.step) * a.H_kv + kvh; };
-  float m = kNegBig;
-  for (int i = threadIdx.x; i < j.n; i += 64 * kJoinWaves) m = fmaxf(m, a.part_ml[2 * at(i)]);
+  int n = (j.n - w + kJoinWaves - 1) / kJoinWaves;  // parts of this wave
+  n = n < 0 ? 0 : (n > kJoinMost ? kJoinMost : n);
+  f32x2_t mine = {kNegBig, 0.f};
+  if (lane < n) mine = *reinterpret_cast<const f32x2_t*>(a.part_ml + 2 * at(w + kJoinWaves * lane));
+  float acc[PL] = {};
+  float m = kNegBig, f = 0.f;
+  constexpr int U = 8;  // outputs in flight
+  for (int t0 = 0; t0 < n; t0 += U) {
+    float po[U][PL];
 #pragma unroll
-  for (int x = 32; x >= 1; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
-  if (lane == 0) red[w] = m;
-  __syncthreads();
+    for (int u = 0; u < U; ++u) {
+      const float* p = a.part_o + at(w + kJoinWaves * (t0 + u < n ? t0 + u : 0)) * D + lane * PL;
 #pragma unroll
-  for (int x = 0; x < kJoinWaves; ++x) m = fmaxf(m, red[x]);
-  float l = 0.f, acc[PL] = {};
-#pragma unroll 8
-  for (int i = w; i < j.n; i += kJoinWaves) {
-    const f32x2_t ml = *reinterpret_cast<const f32x2_t*>(a.part_ml + 2 * at(i));
-    const float* po = a.part_o + at(i) * D + lane * PL;
-    const float f = fast_exp2(ml[0] - m);
-    l = __builtin_fmaf(ml[1], f, l);
+      for (int e = 0; e < PL; ++e) po[u][e] = p[e];
+    }
+    if (t0 == 0) {
+      m = mine[0];
 #pragma unroll
-    for (int e = 0; e < PL; ++e) acc[e] = __builtin_fmaf(po[e], f, acc[e]);
+      for (int x = 32; x >= 1; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+      f = fast_exp2(mine[0] - m);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float g = __shfl(f, t0 + u);
+      if (t0 + u < n) {
+#pragma unroll
+        for (int e = 0; e < PL; ++e) acc[e] = __builtin_fmaf(po[u][e], g, acc[e]);
+      }
+    }
   }
-  if (lane == 0) lpart[w] = l;
+  const float lw = wave_sum(f * mine[1]);
+  if (lane == 0) {
+    ml[w][0] = m;
+    ml[w][1] = lw;
+  }
 #pragma unroll
   for (int e = 0; e < PL; ++e) opart[w][lane * PL + e] = acc[e];
   __syncthreads();
-  l = 0.f;
+  m = kNegBig;
 #pragma unroll
-  for (int x = 0; x < kJoinWaves; ++x) l += lpart[x];
+  for (int x = 0; x < kJoinWaves; ++x) m = fmaxf(m, ml[x][0]);
+  float l = 0.f, wgt[kJoinWaves];
+#pragma unroll
+  for (int x = 0; x < kJoinWaves; ++x) {
+    wgt[x] = fast_exp2(ml[x][0] - m);
+    l = __builtin_fmaf(ml[x][1], wgt[x], l);
+  }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   const int64_t head = kvh * a.G + j.in_group;
   for (int e = threadIdx.x; e < D; e += 64 * kJoinWaves) {
     float o = 0.f;
 #pragma unroll
-    for (int x = 0; x < kJoinWaves; ++x) o += opart[x][e];
+    for (int x = 0; x < kJoinWaves; ++x) o = __builtin_fmaf(opart[x][e], wgt[x], o);
     static_cast<T*>(a.o)[j.q_row * a.ot + head * a.oh + e] = (T)(o * inv);
   }
   if (a.lse != nullptr && threadIdx.x == 0)
     a.lse[head * a.lse_head + j.q_row] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
-template <int D>
-hipError_t launch(const PackedArgs& a, int n_tiles, int n_few, hipStream_t stream) {
-  if (n_tiles > 0)
-    hipLaunchKernelGGL((packed_bf16_kernel<D>), dim3((uint32_t)n_tiles * a.H_kv), dim3(256), 0,
-                       stream, a);
-  if (n_few > 0) {
-    PackedArgs few = a;
-    few.items += n_tiles;
-    hipLaunchKernelGGL((few_bf16_kernel<D>), dim3((uint32_t)n_few * a.H_kv), dim3(256), 0, stream,
-                       few);
-  }
+template <int D, int KINDS>
+void launch_units(const PackedArgs& a, int units, hipStream_t stream) {
+  if (units > 0)
+    hipLaunchKernelGGL((packed_bf16_kernel<D, KINDS>), dim3((uint32_t)units * a.H_kv),
+                       dim3(64 * NW), 0, stream, a);
+}
+
+hipError_t launch_64(const PackedArgs& a, int n_few, hipStream_t stream) {
+  launch_units<64, kTiles>(a, a.n_tiles, stream);
+  PackedArgs few = a;
+  few.items += a.n_tiles;
+  launch_units<64, kFew>(few, n_few, stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_128(const PackedArgs& a, int n_few, hipStream_t stream) {
+  launch_units<128, kTiles | kFew>(a, a.n_tiles + n_few, stream);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_packed_bf16(int d, const PackedArgs& a, int n_tiles, int n_few,
-                              hipStream_t stream) {
-  if (d == 64) return launch<64>(a, n_tiles, n_few, stream);
-  if (d == 128) return launch<128>(a, n_tiles, n_few, stream);
+hipError_t launch_packed_bf16(int d, const PackedArgs& a, int n_few, hipStream_t stream) {
+  if (d == 64) return launch_64(a, n_few, stream);
+  if (d == 128) return launch_128(a, n_few, stream);
   return hipErrorInvalidValue;
 }
 

@@ -333,26 +333,31 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
   }
 }
 
-template <int D>
-hipError_t launch(const PackedArgs& a, int n_tiles, int n_few, hipStream_t stream) {
-  if (n_tiles > 0)
-    hipLaunchKernelGGL((packed_f32_kernel<D, 2>), dim3((uint32_t)n_tiles * a.H_kv),
+template <int D, int RG>
+void launch_units(const PackedArgs& a, int units, hipStream_t stream) {
+  if (units > 0)
+    hipLaunchKernelGGL((packed_f32_kernel<D, RG>), dim3((uint32_t)units * a.H_kv),
                        dim3(64 * kWaves), 0, stream, a);
-  if (n_few > 0) {
-    PackedArgs few = a;
-    few.items += n_tiles;
-    hipLaunchKernelGGL((packed_f32_kernel<D, 1>), dim3((uint32_t)n_few * a.H_kv),
-                       dim3(64 * kWaves), 0, stream, few);
+}
+
+template <int D>
+hipError_t launch(const PackedArgs& a, int n_few, hipStream_t stream) {
+  if (a.tile_rows == kPackedNarrow) {  // tiles and few-row parts alike
+    launch_units<D, 1>(a, a.n_tiles + n_few, stream);
+    return hipGetLastError();
   }
+  launch_units<D, 2>(a, a.n_tiles, stream);
+  PackedArgs few = a;
+  few.items += a.n_tiles;
+  launch_units<D, 1>(few, n_few, stream);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_packed_f32(int d, const PackedArgs& a, int n_tiles, int n_few,
-                             hipStream_t stream) {
-  if (d == 64) return launch<64>(a, n_tiles, n_few, stream);
-  if (d == 128) return launch<128>(a, n_tiles, n_few, stream);
+hipError_t launch_packed_f32(int d, const PackedArgs& a, int n_few, hipStream_t stream) {
+  if (d == 64) return launch<64>(a, n_few, stream);
+  if (d == 128) return launch<128>(a, n_few, stream);
   return hipErrorInvalidValue;
 }
 

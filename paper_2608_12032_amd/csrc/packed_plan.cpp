@@ -21,16 +21,32 @@ int part_keys(bool bf16, int k_len) {
   return (int)(keys < least ? least : keys);
 }
 
+// fp32 units of 32 rows below which a call takes 16.  us in tiles of 16 / of 32, dense:
+// 128 units (1,024 x 4 heads, d = 128) 25.6 / 39.7; 256 47.2 / 40.2 and causal 31.7 / 40.2;
+// 555 410 / 427, at d = 64 200 / 232; 768 255 / 211, at d = 64 119 / 116.
+constexpr int64_t kWideUnits = 640;
+
 struct Counts {
   int64_t tiles, few, joins, part_rows;
 };
 
+// Rows of a call's tiles.  fp32: 16 where tiles of 32 would make few rounds of the
+// machine's 256 CUs; a row's arithmetic is the same in either.
+int tile_rows(const PackedSeqs& s) {
+  if (s.bf16) return kPackedTile[1];
+  int64_t wide = 0;
+  for (int i = 0; i < s.n; ++i) {
+    const int64_t rows = (int64_t)s.q_len[i] * s.G;
+    if (rows > kPackedFew[0]) wide += (rows + kPackedTile[0] - 1) / kPackedTile[0];
+  }
+  return wide * s.H_kv < kWideUnits ? kPackedNarrow : kPackedTile[0];
+}
+
 // Calls tile(item), few(item), join(row) for every unit, in order; returns their number.
 template <typename Tile, typename Few, typename Join>
-Counts walk(const PackedSeqs& s, Tile&& tile, Few&& few, Join&& join) {
+Counts walk(const PackedSeqs& s, int block, Tile&& tile, Few&& few, Join&& join) {
   Counts c = {0, 0, 0, 0};
   int64_t q0 = 0, k0 = 0;
-  const int block = kPackedTile[s.bf16];
   for (int i = 0; i < s.n; ++i) {
     PackedItem it = {};
     it.q0 = s.q_start ? s.q_start[i] : q0;
@@ -82,10 +98,11 @@ Counts walk(const PackedSeqs& s, Tile&& tile, Few&& few, Join&& join) {
 }  // namespace
 
 bool packed_counts(const PackedSeqs& s, PackedCounts* out) {
-  const Counts c = walk(s, [](const PackedItem&) {}, [](const PackedItem&) {},
+  out->tile_rows = tile_rows(s);
+  const Counts c = walk(s, out->tile_rows, [](const PackedItem&) {}, [](const PackedItem&) {},
                         [](const PackedJoin&) {});
   const int64_t most = ((int64_t)1 << 31) / s.H_kv - 1;
-  if (c.tiles > most || c.few > most || c.joins > most || c.part_rows >= ((int64_t)1 << 31))
+  if (c.tiles + c.few > most || c.joins > most || c.part_rows >= ((int64_t)1 << 31))
     return false;
   out->tiles = (int)c.tiles;
   out->few = (int)c.few;
@@ -99,7 +116,7 @@ void packed_fill(const PackedSeqs& s, const PackedCounts& n, void* plan) {
   PackedItem* const few = tiles + n.tiles;
   PackedJoin* const joins = reinterpret_cast<PackedJoin*>(few + n.few);
   int64_t t = 0, f = 0, j = 0;
-  walk(s, [&](const PackedItem& x) { tiles[t++] = x; }, [&](const PackedItem& x) { few[f++] = x; },
+  walk(s, n.tile_rows, [&](const PackedItem& x) { tiles[t++] = x; }, [&](const PackedItem& x) { few[f++] = x; },
        [&](const PackedJoin& x) { joins[j++] = x; });
   // longest first, so that the launch's tail is made of short units; order changes only
   // the schedule.  (std::sort: no allocation)

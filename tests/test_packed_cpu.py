@@ -38,7 +38,8 @@ def test_units_cover_every_row_and_key_once(L, dtype, causal, seed):
     kl = [rng.choice([0, 1, 63, 128, 129, 700, 5000, 50_000]) for _ in ql]
     p = L.losa_packed_plan(ql, kl, 2 * G, 2, dtype, causal=causal, device="cpu")
     tiles, few, joins = units(p)
-    block, most = (128, 32) if dtype == torch.bfloat16 else (32, 16)
+    block, most = p.info.tile_rows, 32 if dtype == torch.bfloat16 else 16
+    assert block in ((128,) if dtype == torch.bfloat16 else (16, 32))
     assert p.q_rows == max([0] + [sum(ql[:i + 1]) for i in range(7) if ql[i]])
     parts = []
     q0 = k0 = 0
@@ -171,7 +172,7 @@ def test_forward_stride_refusals(L):
 
 def test_forward_refuses_what_is_no_info(L):
     info = L.losa_packed_plan([4], [300], 4, 2, torch.bfloat16, device="cpu").info
-    for name, value in (("H", 5), ("H_kv", 0), ("n_tiles", 3), ("bytes", 8), ("dtype", 4), ("n_few", -1)):
+    for name, value in (("H", 5), ("H_kv", 0), ("n_tiles", 3), ("bytes", 8), ("dtype", 4), ("n_few", -1), ("tile_rows", 64)):
         bad = L._PackedInfo.from_buffer_copy(info)
         setattr(bad, name, value)
         assert fwd(L, info=bad) == 2, name
