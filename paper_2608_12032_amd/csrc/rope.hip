@@ -28,6 +28,19 @@ namespace {
 
 constexpr int kWaves = 4;   // waves of a workgroup
 constexpr int kUnroll = 4;  // heads in flight per lane
+// Heads up to which a wave holds a token's for their norm: no barrier, loads not
+// repeated (121 us where the workgroup's waves share them: 138).
+constexpr int kAlone = 16;
+
+// Output bytes of a call from which it is streamed: stores, and bf16 loads of 16 bytes
+// that are not repeated, go past the caches (the L2s hold 32 MiB).  32,760 tokens x 12
+// heads x 128, bf16, one tensor 48.5 -> 41.7 us, q, k, v with one norm over all heads
+// 143 -> 121 (stores alone 134); 55 MB of fp32 29.7 -> 26.8 (its loads too: 29.4).
+constexpr int64_t kStreamBytes = (int64_t)32 << 20;
+
+// Whose norm: each row's; a token's, its heads over the workgroup's waves; a token's, all
+// its heads in one wave.
+enum Norm { kEach, kShared, kOwn };
 
 // Eight values of a row as they lie in memory, in two groups of four.
 template <typename T>
@@ -41,41 +54,52 @@ struct Raw<float> {
   f32x4_t h[2];
 };
 
-// Groups at e0 and e1; neighbours (!HALVES, e1 = e0 + 4) move as 16 bytes.
-template <bool HALVES>
+// Groups at e0 and e1; neighbours (!HALVES, e1 = e0 + 4) move as 16 bytes, past the
+// caches where the call is large and reads them once (ONCE).
+template <bool HALVES, bool ONCE>
 __device__ __forceinline__ Raw<__bf16> load_raw(const __bf16* p, int e0, int e1) {
   Raw<__bf16> r;
   if constexpr (HALVES) {
     r.h[0] = *reinterpret_cast<const bf16x4_t*>(p + e0);
     r.h[1] = *reinterpret_cast<const bf16x4_t*>(p + e1);
   } else {
-    const bf16x8_t v = *reinterpret_cast<const bf16x8_t*>(p + e0);
+    const bf16x8_t* const at = reinterpret_cast<const bf16x8_t*>(p + e0);
+    const bf16x8_t v = ONCE ? __builtin_nontemporal_load(at) : *at;
     r.h[0] = __builtin_shufflevector(v, v, 0, 1, 2, 3);
     r.h[1] = __builtin_shufflevector(v, v, 4, 5, 6, 7);
   }
   return r;
 }
-template <bool HALVES>
+template <bool HALVES, bool ONCE>
 __device__ __forceinline__ Raw<float> load_raw(const float* p, int e0, int e1) {
   Raw<float> r;
   r.h[0] = *reinterpret_cast<const f32x4_t*>(p + e0);
   r.h[1] = *reinterpret_cast<const f32x4_t*>(p + e1);
   return r;
 }
-template <bool HALVES>
+// Stores go past the caches (STREAM) where the call's outputs are too large to stay in
+// them (kStreamBytes).
+template <bool STREAM, typename V>
+__device__ __forceinline__ void put(void* p, V v) {
+  if constexpr (STREAM)
+    __builtin_nontemporal_store(v, static_cast<V*>(p));
+  else
+    *static_cast<V*>(p) = v;
+}
+template <bool HALVES, bool STREAM>
 __device__ __forceinline__ void store_raw(__bf16* p, int e0, int e1, const Raw<__bf16>& r) {
   if constexpr (HALVES) {
-    *reinterpret_cast<bf16x4_t*>(p + e0) = r.h[0];
-    *reinterpret_cast<bf16x4_t*>(p + e1) = r.h[1];
+    put<STREAM, bf16x4_t>(p + e0, r.h[0]);
+    put<STREAM, bf16x4_t>(p + e1, r.h[1]);
   } else {
-    *reinterpret_cast<bf16x8_t*>(p + e0) =
-        __builtin_shufflevector(r.h[0], r.h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    put<STREAM, bf16x8_t>(p + e0,
+                          __builtin_shufflevector(r.h[0], r.h[1], 0, 1, 2, 3, 4, 5, 6, 7));
   }
 }
-template <bool HALVES>
+template <bool HALVES, bool STREAM>
 __device__ __forceinline__ void store_raw(float* p, int e0, int e1, const Raw<float>& r) {
-  *reinterpret_cast<f32x4_t*>(p + e0) = r.h[0];
-  *reinterpret_cast<f32x4_t*>(p + e1) = r.h[1];
+  put<STREAM, f32x4_t>(p + e0, r.h[0]);
+  put<STREAM, f32x4_t>(p + e1, r.h[1]);
 }
 
 template <typename T>
@@ -105,15 +129,18 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-// Workgroup -> tensor, batch, token tile, heads.  One norm over all heads (ALL): a
-// workgroup owns a tile of tokens, its waves take the heads in turn (kUnroll at a
-// time) and add their sums in LDS.  Else a wave owns a tile and `hc` heads, the
-// workgroup's waves neighbouring tiles.
-template <typename T, int D, bool HALVES, bool ALL>
+// Workgroup -> tensor, batch, token tile, heads.  kEach: a wave owns a tile of tokens
+// and `hc` heads, the workgroup's waves neighbouring tiles.  kOwn: the same with all of the
+// 16 heads or fewer, which the wave holds in registers between their sum and their
+// output.  kShared: a workgroup owns a tile, its waves take the heads in turn and add
+// their sums in LDS; with more than 16 heads a pass reads them again.
+template <typename T, int D, bool HALVES, bool STREAM, Norm WHOSE>
 __global__ void __launch_bounds__(64 * kWaves) rows_kernel(const RowsArgs a) {
   constexpr int L = D / 8;    // lanes per row
   constexpr int TW = 64 / L;  // tokens per wave
-  __shared__ float part[ALL ? 2 : 1][kWaves][TW];
+  constexpr bool ALL = WHOSE != kEach, SHARED = WHOSE == kShared;
+  constexpr int U = WHOSE == kOwn ? kAlone : kUnroll;  // heads in flight
+  __shared__ float part[SHARED ? 2 : 1][kWaves][TW];
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int l = lane % L, tk = lane / L;
@@ -121,11 +148,11 @@ __global__ void __launch_bounds__(64 * kWaves) rows_kernel(const RowsArgs a) {
   int64_t j = blockIdx.x;
   while (ti < 2 && j >= a.blocks[ti]) j -= a.blocks[ti++];
   const RowsTensor& t = a.t[ti];
-  const int64_t tw = j / t.chunks;  // tile (ALL) or group of kWaves tiles
+  const int64_t tw = j / t.chunks;  // tile (kShared) or group of kWaves tiles
   const int chunk = (int)(j - tw * t.chunks);
   const int b = (int)(tw / a.tiles);
   const int tile = (int)(tw - (int64_t)b * a.tiles);
-  const int n = (ALL ? tile : tile * kWaves + w) * TW + tk;
+  const int n = (SHARED ? tile : tile * kWaves + w) * TW + tk;
   const bool real = n < a.N;       // else a padding row (0), or none
   const bool there = n < a.n_pad;
   const int nr = real ? n : 0;     // a token whose row and positions may be read
@@ -166,20 +193,32 @@ __global__ void __launch_bounds__(64 * kWaves) rows_kernel(const RowsArgs a) {
 
   const T* xp = static_cast<const T*>(t.x) + b * t.xb + nr * t.xt;
   T* yp = static_cast<T*>(t.y) + b * t.yb + (int64_t)n * t.yt;
-  const int h0 = ALL ? w * kUnroll : chunk * t.hc;
-  const int h1 = ALL ? t.H : (h0 + t.hc < t.H ? h0 + t.hc : t.H);
-  const int step = ALL ? kWaves * kUnroll : kUnroll;  // heads a pass of the loops below
+  const int h0 = SHARED ? w * U : chunk * t.hc;
+  const int h1 = SHARED ? t.H : (h0 + t.hc < t.H ? h0 + t.hc : t.H);
+  const int step = SHARED ? kWaves * U : U;  // heads a pass of the loops below
 
-  Raw<T> raw[kUnroll];
+  Raw<T> raw[U];
   auto load = [&](int h) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
       raw[u] = Raw<T>{};
-      if (h + u < h1 && real) raw[u] = load_raw<HALVES>(xp + (h + u) * t.xh, e0, e1);
+      if (h + u < h1 && real) raw[u] = load_raw<HALVES, STREAM && !SHARED>(xp + (h + u) * t.xh, e0, e1);
     }
   };
   float mean = 0.f, inv = 1.f;
   const bool once = h0 + step >= h1;  // every head of this wave is held in raw
+  // sum of a token's lanes' (and, shared, waves') values, in every lane
+  auto token_sum = [&](float x, int which) {
+    x = row_sum<L>(x);
+    if constexpr (SHARED) {
+      if (l == 0) part[which][w][tk] = x;
+      __syncthreads();
+      x = 0.f;
+#pragma unroll
+      for (int y = 0; y < kWaves; ++y) x += part[which][y][tk];
+    }
+    return x;
+  };
   if constexpr (ALL) {
     if (t.norm != kNormNone) {
       if (once) load(h0);
@@ -189,24 +228,19 @@ __global__ void __launch_bounds__(64 * kWaves) rows_kernel(const RowsArgs a) {
         for (int h = h0; h < h1; h += step) {
           if (!once) load(h);
 #pragma unroll
-          for (int u = 0; u < kUnroll; ++u) {
+          for (int u = 0; u < U; ++u) {
             float x[8];
             widen<T>(raw[u], x);
             sum += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
           }
         }
-        sum = row_sum<L>(sum);
-        if (l == 0) part[0][w][tk] = sum;
-        __syncthreads();
-#pragma unroll
-        for (int y = 0; y < kWaves; ++y) mean += part[0][y][tk];
-        mean /= count;
+        mean = token_sum(sum, 0) / count;
       }
       float sq = 0.f;
       for (int h = h0; h < h1; h += step) {
         if (!once) load(h);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
+        for (int u = 0; u < U; ++u) {
           float x[8];
           widen<T>(raw[u], x);
           if (h + u < h1) {
@@ -218,13 +252,7 @@ __global__ void __launch_bounds__(64 * kWaves) rows_kernel(const RowsArgs a) {
           }
         }
       }
-      sq = row_sum<L>(sq);
-      if (l == 0) part[1][w][tk] = sq;
-      __syncthreads();
-      float total = 0.f;
-#pragma unroll
-      for (int y = 0; y < kWaves; ++y) total += part[1][y][tk];
-      inv = 1.0f / sqrtf(total / count + a.eps);
+      inv = 1.0f / sqrtf(token_sum(sq, 1) / count + a.eps);
     }
   }
 
@@ -246,7 +274,7 @@ __global__ void __launch_bounds__(64 * kWaves) rows_kernel(const RowsArgs a) {
   for (int h = h0; h < h1; h += step) {
     if (!(ALL && once && t.norm != kNormNone)) load(h);
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
       if (h + u >= h1) break;
       if (t.norm != kNormNone || t.rotate) {
         float x[8];
@@ -288,7 +316,7 @@ __global__ void __launch_bounds__(64 * kWaves) rows_kernel(const RowsArgs a) {
         raw[u] = narrow<T>(x);
         if (!real) raw[u] = Raw<T>{};
       }
-      if (there) store_raw<HALVES>(yp + (h + u) * t.yh, e0, e1, raw[u]);
+      if (there) store_raw<HALVES, STREAM>(yp + (h + u) * t.yh, e0, e1, raw[u]);
     }
   }
 }
@@ -301,33 +329,43 @@ int heads_per_wave(int H, int64_t groups_heads) {
   return (hc + kUnroll - 1) / kUnroll * kUnroll;
 }
 
+template <typename T, int D, bool HALVES, bool STREAM>
+void launch_rows_of(const RowsArgs& a, Norm whose, uint32_t groups, hipStream_t stream) {
+  const dim3 grid(groups), block(64 * kWaves);
+  if (whose == kEach)
+    hipLaunchKernelGGL((rows_kernel<T, D, HALVES, STREAM, kEach>), grid, block, 0, stream, a);
+  else if (whose == kOwn)
+    hipLaunchKernelGGL((rows_kernel<T, D, HALVES, STREAM, kOwn>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((rows_kernel<T, D, HALVES, STREAM, kShared>), grid, block, 0, stream, a);
+}
+
 template <typename T, int D, bool HALVES>
 hipError_t launch(RowsArgs& a, int tensors, bool all, hipStream_t stream) {
   constexpr int TW = 64 / (D / 8);
-  const int64_t tiles = (a.n_pad + TW - 1) / TW;
-  a.tiles = (int)(all ? tiles : (tiles + kWaves - 1) / kWaves);
   int64_t heads = 0, total = 0;
-  for (int i = 0; i < tensors; ++i) heads += a.t[i].H;
+  int normed = 0;  // most heads of a tensor with a norm
+  for (int i = 0; i < tensors; ++i) {
+    heads += a.t[i].H;
+    if (a.t[i].norm != kNormNone && a.t[i].H > normed) normed = a.t[i].H;
+  }
+  const Norm whose = !all || normed == 0 ? kEach : (normed <= kAlone ? kOwn : kShared);
+  const int64_t tiles = (a.n_pad + TW - 1) / TW;
+  a.tiles = (int)(whose == kShared ? tiles : (tiles + kWaves - 1) / kWaves);
   for (int i = 0; i < 3; ++i) {
     a.blocks[i] = 0;
     if (i >= tensors) continue;
     RowsTensor& t = a.t[i];
-    t.hc = t.H;
-    t.chunks = 1;
-    if (!all) {
-      t.hc = heads_per_wave(t.H, heads * a.B * a.tiles);
-      t.chunks = (t.H + t.hc - 1) / t.hc;
-    }
+    t.hc = whose == kEach ? heads_per_wave(t.H, heads * a.B * a.tiles) : t.H;
+    t.chunks = (t.H + t.hc - 1) / t.hc;
     a.blocks[i] = (int64_t)a.B * a.tiles * t.chunks;
     total += a.blocks[i];
   }
   if (total >= ((int64_t)1 << 31)) return hipErrorInvalidConfiguration;
-  if (all)
-    hipLaunchKernelGGL((rows_kernel<T, D, HALVES, true>), dim3((uint32_t)total),
-                       dim3(64 * kWaves), 0, stream, a);
+  if (heads * a.B * a.n_pad * D * (int64_t)sizeof(T) >= kStreamBytes)
+    launch_rows_of<T, D, HALVES, true>(a, whose, (uint32_t)total, stream);
   else
-    hipLaunchKernelGGL((rows_kernel<T, D, HALVES, false>), dim3((uint32_t)total),
-                       dim3(64 * kWaves), 0, stream, a);
+    launch_rows_of<T, D, HALVES, false>(a, whose, (uint32_t)total, stream);
   return hipGetLastError();
 }
 
