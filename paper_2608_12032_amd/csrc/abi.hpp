@@ -19,9 +19,10 @@ inline losa_status hip_status(hipError_t e, const char* what) {
 
 inline size_t elem_bytes(losa_dtype dt) { return dt == LOSA_DTYPE_BF16 ? 2 : 4; }
 
-// A view of [B][N][H] rows of d elements of `el` bytes.  Fails on what the kernels
-// cannot address; rows of an output must not overlap.
-losa_status check_view(const char* name, const losa_view* v, int el, int B, int64_t N, int H, int d,
-                       bool out);
+// Takes a view of [B][N][H] rows of d elements of `el` bytes: *to is `from` with the
+// strides that are never used, those along one element, set to d.  Fails on what the
+// kernels cannot address; rows of an output must not overlap.
+losa_status take_view(const char* name, const losa_view* from, losa_view* to, int el, int B,
+                      int64_t N, int H, int d, bool out);
 
 }  // namespace losa

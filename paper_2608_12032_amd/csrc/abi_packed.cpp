@@ -11,10 +11,10 @@
 namespace {
 
 using losa::aligned16;
-using losa::check_view;
 using losa::elem_bytes;
 using losa::fail;
 using losa::hip_status;
+using losa::take_view;
 
 // The two sequences of `s` that own the same row of q, if any (an index pair).
 losa_status check_disjoint(const int64_t* start, const int32_t* len, int n) {
@@ -126,16 +126,17 @@ losa_status losa_packed_attn_fwd(const losa_view* q, const losa_view* k, const l
   const bool bf16 = info->dtype == LOSA_DTYPE_BF16;
   const int el = (int)elem_bytes(info->dtype);
   losa_status st;
-  if ((st = check_view("q", q, el, 1, q_rows, info->H, d, false)) != LOSA_OK) return st;
-  if ((st = check_view("o", o, el, 1, q_rows, info->H, d, true)) != LOSA_OK) return st;
+  losa_view qv, kv[2] = {}, ov;
+  if ((st = take_view("q", q, &qv, el, 1, q_rows, info->H, d, false)) != LOSA_OK) return st;
+  if ((st = take_view("o", o, &ov, el, 1, q_rows, info->H, d, true)) != LOSA_OK) return st;
   if (info->k_rows > 0) {
-    const losa_view* kv[2] = {k, v};
     for (int i = 0; i < 2; ++i) {
-      const char* name = i == 0 ? "k" : "v";
-      if ((st = check_view(name, kv[i], el, 1, k_rows, info->H_kv, d, false)) != LOSA_OK) return st;
-      if (k_rows > 1 && (kv[i]->token < d || kv[i]->token * el > ((int64_t)1 << 26)))
+      const char* const name = i == 0 ? "k" : "v";
+      st = take_view(name, i == 0 ? k : v, &kv[i], el, 1, k_rows, info->H_kv, d, false);
+      if (st != LOSA_OK) return st;
+      if (kv[i].token < d || kv[i].token * el > ((int64_t)1 << 26))
         return fail(LOSA_ERR_INVALID_SHAPE, "%s: token stride %lld not in [d, 64 MiB]", name,
-                    (long long)kv[i]->token);
+                    (long long)kv[i].token);
     }
   }
   if (lse) {
@@ -155,21 +156,21 @@ losa_status losa_packed_attn_fwd(const losa_view* q, const losa_view* k, const l
   losa::PackedArgs a = {};
   a.items = static_cast<const losa::PackedItem*>(plan);
   a.joins = reinterpret_cast<const losa::PackedJoin*>(a.items + info->n_tiles + info->n_few);
-  a.q = q->data;
-  a.k = k->data;
-  a.v = v->data;
-  a.o = o->data;
+  a.q = qv.data;
+  a.k = kv[0].data;
+  a.v = kv[1].data;
+  a.o = ov.data;
   a.lse = lse;
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = a.part_o + (size_t)info->part_rows * info->H_kv * d;
-  a.qt = q->token;
-  a.qh = q->head;
-  a.kt = k->token;
-  a.kh = k->head;
-  a.vt = v->token;
-  a.vh = v->head;
-  a.ot = o->token;
-  a.oh = o->head;
+  a.qt = qv.token;
+  a.qh = qv.head;
+  a.kt = kv[0].token;
+  a.kh = kv[0].head;
+  a.vt = kv[1].token;
+  a.vh = kv[1].head;
+  a.ot = ov.token;
+  a.oh = ov.head;
   a.lse_head = lse_head;
   a.q_rows = q_rows;
   a.k_rows = k_rows;

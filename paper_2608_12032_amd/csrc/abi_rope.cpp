@@ -7,31 +7,36 @@
 #include "abi.hpp"
 #include "rope.hpp"
 
-losa_status losa::check_view(const char* name, const losa_view* v, int el, int B, int64_t N, int H, int d,
-                       bool out) {
-  if (!v || !v->data) return fail(LOSA_ERR_NULL_POINTER, "%s must be non-NULL", name);
-  const int64_t s[3] = {v->batch, v->token, v->head};
+losa_status losa::take_view(const char* name, const losa_view* from, losa_view* to, int el, int B,
+                            int64_t N, int H, int d, bool out) {
+  if (!from || !from->data) return fail(LOSA_ERR_NULL_POINTER, "%s must be non-NULL", name);
+  *to = *from;
+  int64_t* const s[3] = {&to->batch, &to->token, &to->head};
   const int64_t n[3] = {B, N, H};
   for (int i = 0; i < 3; ++i) {
-    if (s[i] < 0 || s[i] >= ((int64_t)1 << 40))
-      return fail(LOSA_ERR_INVALID_SHAPE, "%s: stride %lld out of range", name, (long long)s[i]);
-    if (s[i] * el % 16 != 0)
+    if (n[i] <= 1) {
+      *s[i] = d;
+      continue;
+    }
+    if (*s[i] < 0 || *s[i] >= ((int64_t)1 << 40))
+      return fail(LOSA_ERR_INVALID_SHAPE, "%s: stride %lld out of range", name, (long long)*s[i]);
+    if (*s[i] * el % 16 != 0)
       return fail(LOSA_ERR_ALIGNMENT, "%s: strides must be multiples of 16 bytes", name);
-    if (out && n[i] > 1 && s[i] < d)
+    if (out && *s[i] < d)
       return fail(LOSA_ERR_INVALID_SHAPE, "%s: rows of an output overlap (stride %lld < d=%d)",
-                  name, (long long)s[i], d);
+                  name, (long long)*s[i], d);
   }
-  if (!aligned16(v->data)) return fail(LOSA_ERR_ALIGNMENT, "%s must be 16-byte aligned", name);
+  if (!aligned16(to->data)) return fail(LOSA_ERR_ALIGNMENT, "%s must be 16-byte aligned", name);
   return LOSA_OK;
 }
 
 namespace {
 
 using losa::aligned16;
-using losa::check_view;
 using losa::elem_bytes;
 using losa::fail;
 using losa::hip_status;
+using losa::take_view;
 
 losa_status check_rows(losa_dtype dtype, int B, int N, int N_pad, int H, int d) {
   if (B <= 0 || N <= 0 || H <= 0 || d <= 0)
@@ -100,15 +105,15 @@ losa_status check_rotation(const losa_rotation* r, int N, int d, losa::RowsArgs*
   return LOSA_OK;
 }
 
-void set_tensor(losa::RowsTensor* t, const losa_view* x, const losa_view* y, int H) {
-  t->x = x->data;
-  t->xb = x->batch;
-  t->xt = x->token;
-  t->xh = x->head;
-  t->y = y->data;
-  t->yb = y->batch;
-  t->yt = y->token;
-  t->yh = y->head;
+void set_tensor(losa::RowsTensor* t, const losa_view& x, const losa_view& y, int H) {
+  t->x = x.data;
+  t->xb = x.batch;
+  t->xt = x.token;
+  t->xh = x.head;
+  t->y = y.data;
+  t->yb = y.batch;
+  t->yt = y.token;
+  t->yh = y.head;
   t->H = H;
 }
 
@@ -145,14 +150,15 @@ losa_status losa_rope(const losa_view* x, losa_dtype dtype, int B, int N, int N_
   losa_status st = check_rows(dtype, B, N, N_pad, H, d);
   if (st != LOSA_OK) return st;
   const int el = (int)elem_bytes(dtype);
-  if ((st = check_view("x", x, el, B, N, H, d, false)) != LOSA_OK) return st;
-  if ((st = check_view("y", y, el, B, N_pad, H, d, true)) != LOSA_OK) return st;
+  losa_view xv, yv;
+  if ((st = take_view("x", x, &xv, el, B, N, H, d, false)) != LOSA_OK) return st;
+  if ((st = take_view("y", y, &yv, el, B, N_pad, H, d, true)) != LOSA_OK) return st;
   losa::RowsArgs a = {};
   if ((st = check_rotation(rot, N, d, &a)) != LOSA_OK) return st;
   a.B = B;
   a.N = N;
   a.n_pad = N_pad;
-  set_tensor(&a.t[0], x, y, H);
+  set_tensor(&a.t[0], xv, yv, H);
   a.t[0].rotate = 1;
   return hip_status(losa::launch_rows(d, dtype == LOSA_DTYPE_BF16,
                                       rot->pairs == LOSA_PAIRS_HALVES, a, 1, false,
@@ -169,15 +175,16 @@ losa_status losa_qk_norm_rope(const losa_view* q, const losa_view* k, const losa
   if (st != LOSA_OK) return st;
   if ((st = check_rows(dtype, B, N, N_pad, H_kv, d)) != LOSA_OK) return st;
   const int el = (int)elem_bytes(dtype);
-  if ((st = check_view("q", q, el, B, N, H, d, false)) != LOSA_OK) return st;
-  if ((st = check_view("k", k, el, B, N, H_kv, d, false)) != LOSA_OK) return st;
-  if ((st = check_view("q_out", q_out, el, B, N_pad, H, d, true)) != LOSA_OK) return st;
-  if ((st = check_view("k_out", k_out, el, B, N_pad, H_kv, d, true)) != LOSA_OK) return st;
+  losa_view in[3], to[3];
+  if ((st = take_view("q", q, &in[0], el, B, N, H, d, false)) != LOSA_OK) return st;
+  if ((st = take_view("k", k, &in[1], el, B, N, H_kv, d, false)) != LOSA_OK) return st;
+  if ((st = take_view("q_out", q_out, &to[0], el, B, N_pad, H, d, true)) != LOSA_OK) return st;
+  if ((st = take_view("k_out", k_out, &to[1], el, B, N_pad, H_kv, d, true)) != LOSA_OK) return st;
   if ((v == nullptr) != (v_out == nullptr))
     return fail(LOSA_ERR_NULL_POINTER, "v and v_out must both be given or both be NULL");
   if (v) {
-    if ((st = check_view("v", v, el, B, N, H_kv, d, false)) != LOSA_OK) return st;
-    if ((st = check_view("v_out", v_out, el, B, N_pad, H_kv, d, true)) != LOSA_OK) return st;
+    if ((st = take_view("v", v, &in[2], el, B, N, H_kv, d, false)) != LOSA_OK) return st;
+    if ((st = take_view("v_out", v_out, &to[2], el, B, N_pad, H_kv, d, true)) != LOSA_OK) return st;
   }
   losa::RowsArgs a = {};
   if (rot && (st = check_rotation(rot, N, d, &a)) != LOSA_OK) return st;
@@ -195,9 +202,9 @@ losa_status losa_qk_norm_rope(const losa_view* q, const losa_view* k, const losa
   a.B = B;
   a.N = N;
   a.n_pad = N_pad;
-  set_tensor(&a.t[0], q, q_out, H);
-  set_tensor(&a.t[1], k, k_out, H_kv);
-  if (v) set_tensor(&a.t[2], v, v_out, H_kv);
+  set_tensor(&a.t[0], in[0], to[0], H);
+  set_tensor(&a.t[1], in[1], to[1], H_kv);
+  if (v) set_tensor(&a.t[2], in[2], to[2], H_kv);
   a.t[0].rotate = a.t[1].rotate = rot != nullptr;
   if (norm) {
     a.eps = norm->eps;

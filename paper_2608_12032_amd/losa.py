@@ -11,6 +11,7 @@ import ctypes
 import functools
 import math
 import os
+import struct
 
 import torch
 
@@ -41,24 +42,13 @@ NORMS = {"rms": 1, "layer": 2}
 MAX_AXES = 4
 
 
-class _View(ctypes.Structure):
-    """losa_view"""
-    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64),
-                ("head", ctypes.c_int64)]
-
-
-class _Rotation(ctypes.Structure):
-    """losa_rotation"""
-    _fields_ = [("n_axes", ctypes.c_int), ("axis_dim", ctypes.c_int * MAX_AXES),
-                ("axis_len", ctypes.c_int * MAX_AXES), ("table", ctypes.c_void_p),
-                ("pos", ctypes.c_void_p), ("pos_batch", ctypes.c_int64), ("pairs", ctypes.c_int)]
-
-
-class _QkNorm(ctypes.Structure):
-    """losa_qk_norm_args"""
-    _fields_ = [("kind", ctypes.c_int), ("all_heads", ctypes.c_int), ("eps", ctypes.c_float),
-                ("q_weight", ctypes.c_void_p), ("q_bias", ctypes.c_void_p),
-                ("k_weight", ctypes.c_void_p), ("k_bias", ctypes.c_void_p)]
+# Structures of the C ABI as bytes, which ctypes passes by address: losa_view (data, batch,
+# token, head), losa_rotation (n_axes, axis_dim, axis_len; table, pos, pos_batch, pairs) and
+# losa_qk_norm_args (kind, all_heads, eps; weights and biases)
+_VIEW = struct.Struct("@Qqqq").pack
+_AXES = struct.Struct("@9i4x").pack
+_ROTATION = struct.Struct("@QQqi4x").pack
+_QK_NORM = struct.Struct("@iif4xQQQQ").pack
 
 
 class _PackedInfo(ctypes.Structure):
@@ -430,8 +420,9 @@ class RopeTable:
 
     def __init__(self, data, axis_dim, axis_len):
         self.data, self.axis_dim, self.axis_len = data, tuple(axis_dim), tuple(axis_len)
-        n, ints = len(self.axis_dim), ctypes.c_int * MAX_AXES
-        self._form = _Rotation(n, ints(*self.axis_dim), ints(*self.axis_len))
+        self._axes = len(self.axis_dim)
+        rest = (0,) * (MAX_AXES - self._axes)
+        self._head = _AXES(self._axes, *self.axis_dim, *rest, *self.axis_len, *rest)
         self._floats = sum(a * b for a, b in zip(self.axis_dim, self.axis_len))
 
 
@@ -452,43 +443,56 @@ def losa_rope_table(axis_dim, axis_len, base: float = 10000.0, device="cuda") ->
     return RopeTable(host.to(device), axis_dim, axis_len)
 
 
-def _view(t, name, device, dtype, shape, swap=False):
-    """losa_view of a [B, N, H, d] tensor (swap: [B, H, N, d]) of this shape, whose rows
-    of d are contiguous."""
-    if not (isinstance(t, torch.Tensor) and t.device == device and t.is_cuda and t.dtype == dtype
-            and t.shape == shape):
-        if not isinstance(t, torch.Tensor):
-            raise TypeError(f"{name} must be a torch.Tensor")
-        if not t.is_cuda or t.device != device:
-            raise ValueError(f"{name} must live on {device} (got {t.device})")
-        if t.dtype != dtype:
-            raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
+def _wrong(t, name, device, dtype, shape):
+    """Raises what is wrong with a view's tensor."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} must live on {device} (got {t.device})")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
+    if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
-    sb, sn, sh, sd = t.stride()
-    if sd != 1:
-        raise ValueError(f"{name} must have contiguous rows (stride 1 in the last dim)")
-    # (a stride along one element is never used, and torch may set it to anything)
-    B, N, H, _ = shape
-    sb, sn, sh = sb if B > 1 else 0, sn if N > 1 else 0, sh if H > 1 else 0
-    return _View(t.data_ptr(), sb, sh, sn) if swap else _View(t.data_ptr(), sb, sn, sh)
+    raise ValueError(f"{name} must have contiguous rows (stride 1 in the last dim)")
+
+
+def _view(t, name, device, dtype, shape):
+    """losa_view of a [B, N, H, d] tensor of this shape whose rows of d are contiguous."""
+    if (isinstance(t, torch.Tensor) and t.device == device and t.dtype == dtype
+            and t.shape == shape):
+        sb, sn, sh, sd = t.stride()
+        if sd == 1 and t.is_cuda:
+            return _VIEW(t.data_ptr(), sb, sn, sh)
+    _wrong(t, name, device, dtype, shape)
+
+
+def _view_out(t, name, device, dtype, shape):
+    """losa_view, as of [B, N, H, d], of a [B, H, N, d] tensor."""
+    if (isinstance(t, torch.Tensor) and t.device == device and t.dtype == dtype
+            and t.shape == shape):
+        sb, sh, sn, sd = t.stride()
+        if sd == 1:
+            return _VIEW(t.data_ptr(), sb, sn, sh)
+    _wrong(t, name, device, dtype, shape)
 
 
 def _rotation(table, pos, pairing, B, N, device):
     """losa_rotation of a table and positions int32 [axes, N] or [B, axes, N]."""
     if not isinstance(table, RopeTable):
         raise TypeError("table must be a RopeTable (losa_rope_table)")
-    n = len(table.axis_dim)
-    _arg(table.data, "table", device, dtype=torch.float32, numel=table._floats)
+    n, data = table._axes, table.data
+    _arg(data, "table", device, dtype=torch.float32, numel=table._floats)
     _arg(pos, "pos", device, dtype=torch.int32)
-    if pos.shape != (n, N) and pos.shape != (B, n, N):
-        raise ValueError(f"pos must have shape {(n, N)} or {(B, n, N)} (got {tuple(pos.shape)})")
+    shape = pos.shape
+    if shape == (n, N):
+        batch = 0
+    elif shape == (B, n, N):
+        batch = n * N
+    else:
+        raise ValueError(f"pos must have shape {(n, N)} or {(B, n, N)} (got {tuple(shape)})")
     if pairing not in PAIRS:
         raise ValueError(f"pairing must be one of {tuple(PAIRS)} (got {pairing!r})")
-    rot = _Rotation.from_buffer_copy(table._form)
-    rot.table, rot.pos, rot.pairs = table.data.data_ptr(), pos.data_ptr(), PAIRS[pairing]
-    if pos.dim() == 3:
-        rot.pos_batch = n * N
-    return rot
+    return table._head + _ROTATION(data.data_ptr(), pos.data_ptr(), batch, PAIRS[pairing])
 
 
 def _rows_in(t, name):
@@ -497,19 +501,9 @@ def _rows_in(t, name):
     return t.shape
 
 
-def _rows_out(out, name, x, n_pad):
-    """The output [B, H, n_pad, d] for x [B, N, H, d], and its losa_view."""
-    B, _, H, d = x.shape
-    if out is None:
-        out = torch.empty((B, H, n_pad, d), dtype=x.dtype, device=x.device)
-    elif not isinstance(out, torch.Tensor) or out.dim() != 4:
-        raise ValueError(f"{name} must be a [B, H, n_pad, d] tensor")
-    return out, _view(out, name, x.device, x.dtype, (B, H, n_pad, d), swap=True)
-
-
 def _call(device, fn, *args):
     """fn(*args, stream) on the device's current stream, with that device current."""
-    if torch.cuda.current_device() == device.index:
+    if torch._C._cuda_getDevice() == device.index:
         return fn(*args, _stream(device))
     with torch.cuda.device(device):
         return fn(*args, _stream(device))
@@ -520,14 +514,17 @@ def losa_rope(x, table: RopeTable, pos, n_pad: int | None = None, pairing: str =
     """Rotary positions of x [B, N, H, d] (any strides, rows of d contiguous) ->
     [B, H, n_pad, d], rows from N on 0.  ``pos`` int32 [axes, N] or [B, axes, N];
     ``out`` may have any strides, and may be x's own memory."""
-    B, N, H, d = _rows_in(x, "x")
+    shape = B, N, H, d = _rows_in(x, "x")
     n_pad = N if n_pad is None else n_pad
-    dev, dcode, at = x.device, _dtype_code(x), ctypes.addressof
-    xv = _view(x, "x", dev, x.dtype, x.shape)
+    dev, dt, code = x.device, x.dtype, _dtype_code(x)
+    xv = _view(x, "x", dev, dt, shape)
     rot = _rotation(table, pos, pairing, B, N, dev)
-    out, yv = _rows_out(out, "out", x, n_pad)
-    _check(_call(dev, lib.losa_rope, at(xv), dcode, B, N, n_pad, H, d, at(rot), at(yv)),
-           "losa_rope")
+    if out is None:
+        out = torch.empty((B, H, n_pad, d), dtype=dt, device=dev)
+    yv = _view_out(out, "out", dev, dt, (B, H, n_pad, d))
+    st = _call(dev, lib.losa_rope, xv, code, B, N, n_pad, H, d, rot, yv)
+    if st:
+        _check(st, "losa_rope")
     return out
 
 
@@ -539,27 +536,27 @@ def losa_qk_norm_rope(q, k, v=None, *, norm: str | None = "rms", over: str = "he
     token's heads ("all"), then their rotary positions, in one pass; v beside them ->
     (q, k) or (q, k, v), each [B, heads, n_pad, d].  Inputs and outputs may have any
     strides; weights and biases fp32 of d or heads * d elements."""
-    B, N, H, d = _rows_in(q, "q")
+    shape = B, N, H, d = _rows_in(q, "q")
     Hkv = _rows_in(k, "k")[2]
-    dev, dt, at = q.device, q.dtype, ctypes.addressof
+    dev, dt, code = q.device, q.dtype, _dtype_code(q)
+    shape_kv = (B, N, Hkv, d)
     n_pad = N if n_pad is None else n_pad
-    dcode = _dtype_code(q)
     if over not in ("head", "all"):
         raise ValueError(f"over must be 'head' or 'all' (got {over!r})")
-    qi, ki = _view(q, "q", dev, dt, q.shape), _view(k, "k", dev, dt, (B, N, Hkv, d))
-    vi = None if v is None else _view(v, "v", dev, dt, (B, N, Hkv, d))
+    qi, ki = _view(q, "q", dev, dt, shape), _view(k, "k", dev, dt, shape_kv)
+    vi = None if v is None else _view(v, "v", dev, dt, shape_kv)
     args = None
     if norm is not None:
         if norm not in NORMS:
             raise ValueError(f"norm must be None or one of {tuple(NORMS)} (got {norm!r})")
-        all_heads = over == "all"
-        span, span_kv = (H * d, Hkv * d) if all_heads else (d, d)
+        every = over == "all"
+        span, span_kv = (H * d, Hkv * d) if every else (d, d)
+        at = []
         for name, t, n in (("q_weight", q_weight, span), ("q_bias", q_bias, span),
                            ("k_weight", k_weight, span_kv), ("k_bias", k_bias, span_kv)):
-            if t is not None:
-                _arg(t, name, dev, dtype=torch.float32, shape=(n,))
-        args = _QkNorm(NORMS[norm], all_heads, eps, _ptr(q_weight), _ptr(q_bias), _ptr(k_weight),
-                       _ptr(k_bias))
+            at.append(0 if t is None else
+                      _arg(t, name, dev, dtype=torch.float32, shape=(n,)).data_ptr())
+        args = _QK_NORM(NORMS[norm], every, eps, *at)
     elif not (q_weight is q_bias is k_weight is k_bias is None):
         raise ValueError("weights and biases need a norm")
     if (table is None) != (pos is None):
@@ -567,13 +564,22 @@ def losa_qk_norm_rope(q, k, v=None, *, norm: str | None = "rms", over: str = "he
     rot = None if table is None else _rotation(table, pos, pairing, B, N, dev)
     if v is None and v_out is not None:
         raise ValueError("v_out needs v")
-    q_out, qo = _rows_out(q_out, "q_out", q, n_pad)
-    k_out, ko = _rows_out(k_out, "k_out", k, n_pad)
+    shape, shape_kv = (B, H, n_pad, d), (B, Hkv, n_pad, d)
+    if q_out is None:
+        q_out = torch.empty(shape, dtype=dt, device=dev)
+    if k_out is None:
+        k_out = torch.empty(shape_kv, dtype=dt, device=dev)
+    qo = _view_out(q_out, "q_out", dev, dt, shape)
+    ko = _view_out(k_out, "k_out", dev, dt, shape_kv)
+    vo = None
     if v is not None:
-        v_out, vo = _rows_out(v_out, "v_out", v, n_pad)
-    st = _call(dev, lib.losa_qk_norm_rope, at(qi), at(ki), vi and at(vi), dcode, B, N, n_pad, H,
-               Hkv, d, args and at(args), rot and at(rot), at(qo), at(ko), vi and at(vo))
-    _check(st, "losa_qk_norm_rope")
+        if v_out is None:
+            v_out = torch.empty(shape_kv, dtype=dt, device=dev)
+        vo = _view_out(v_out, "v_out", dev, dt, shape_kv)
+    st = _call(dev, lib.losa_qk_norm_rope, qi, ki, vi, code, B, N, n_pad, H, Hkv, d, args, rot, qo,
+               ko, vo)
+    if st:
+        _check(st, "losa_qk_norm_rope")
     return (q_out, k_out) if v is None else (q_out, k_out, v_out)
 
 
@@ -631,24 +637,14 @@ def losa_packed_plan(q_lens, k_lens, heads: int, kv_heads: int, dtype, causal: b
     return PackedPlan(info, host.to(device), dtype)
 
 
-def _packed_view(t, name, device, dtype, rows, heads, d):
-    """losa_view of a [rows, heads, d] tensor (rows None: any number of them) whose rows
-    of d are contiguous."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 3:
-        raise ValueError(f"{name} must be a [rows, heads, d] tensor")
-    shape = t.shape
-    if not (t.device == device and t.is_cuda and t.dtype == dtype and shape[1] == heads
-            and shape[2] == d and (rows is None or shape[0] == rows)):
-        if not t.is_cuda or t.device != device:
-            raise ValueError(f"{name} must live on {device} (got {t.device})")
-        if t.dtype != dtype:
-            raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
-        raise ValueError(f"{name} must have shape {('any' if rows is None else rows, heads, d)} "
-                         f"(got {tuple(shape)})")
-    sn, sh, sd = t.stride()
-    if sd != 1:
-        raise ValueError(f"{name} must have contiguous rows (stride 1 in the last dim)")
-    return _View(t.data_ptr(), 0, sn if shape[0] > 1 else 0, sh if heads > 1 else 0)
+def _packed_view(t, name, device, dtype, shape):
+    """losa_view of a [rows, heads, d] tensor of this shape whose rows of d are contiguous."""
+    if (isinstance(t, torch.Tensor) and t.device == device and t.dtype == dtype
+            and t.shape == shape):
+        sn, sh, sd = t.stride()
+        if sd == 1:
+            return _VIEW(t.data_ptr(), 0, sn, sh)
+    _wrong(t, name, device, dtype, shape)
 
 
 def losa_packed_attn_fwd(q, k, v, plan: PackedPlan, scale: float | None = None,
@@ -658,35 +654,40 @@ def losa_packed_attn_fwd(q, k, v, plan: PackedPlan, scale: float | None = None,
     of ``out`` and ``lse`` that no sequence owns are left as they are."""
     if not isinstance(plan, PackedPlan):
         raise TypeError("plan must be a PackedPlan (losa_packed_plan)")
-    if not isinstance(q, torch.Tensor) or q.dim() != 3:
-        raise ValueError("q must be a [rows, heads, d] tensor")
+    for name, t in (("q", q), ("k", k)):
+        if not isinstance(t, torch.Tensor) or t.dim() != 3:
+            raise ValueError(f"{name} must be a [rows, heads, d] tensor")
     rows, _, d = q.shape
-    dev, dt, at = q.device, plan.dtype, ctypes.addressof
-    if plan.data.device != dev:
-        raise ValueError(f"q and the plan must live on one device (got {dev}, {plan.data.device})")
-    qv = _packed_view(q, "q", dev, dt, None, plan.heads, d)
-    kv = _packed_view(k, "k", dev, dt, None, plan.kv_heads, d)
-    vv = _packed_view(v, "v", dev, dt, None, plan.kv_heads, d)
     k_rows = k.shape[0]
-    if k_rows != v.shape[0]:
-        raise ValueError(f"k has {k_rows} rows, v {v.shape[0]}")
+    dev, dt = q.device, plan.dtype
+    shape, shape_kv = (rows, plan.heads, d), (k_rows, plan.kv_heads, d)
+    if not q.is_cuda:
+        raise ValueError(f"q must live on a GPU (got {dev})")
+    if plan.data.device != dev:
+        raise ValueError(f"the plan must live on {dev} (got {plan.data.device})")
+    qv = _packed_view(q, "q", dev, dt, shape)
+    kv = _packed_view(k, "k", dev, dt, shape_kv)
+    vv = _packed_view(v, "v", dev, dt, shape_kv)
     if out is None:
-        out = torch.empty((rows, plan.heads, d), dtype=dt, device=dev)
-    ov = _packed_view(out, "out", dev, dt, rows, plan.heads, d)
+        out = torch.empty(shape, dtype=dt, device=dev)
+    ov = _packed_view(out, "out", dev, dt, shape)
+    lse_at = None
     if want_lse:
         if lse is None:
             lse = torch.empty((plan.heads, rows), dtype=torch.float32, device=dev)
-        _arg(lse, "lse", dev, dtype=torch.float32, shape=(plan.heads, rows))
+        lse_at = _arg(lse, "lse", dev, dtype=torch.float32, shape=(plan.heads, rows)).data_ptr()
     need = plan.workspace_bytes(d)
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    ws_bytes = 0
+    ws_at, ws_bytes = None, 0
     if workspace is not None:
-        ws_bytes = _arg(workspace, "workspace", dev, nbytes=need).nbytes
-    st = _call(dev, lib.losa_packed_attn_fwd, at(qv), at(kv), at(vv), rows, k_rows, plan._at,
-               plan.data.data_ptr(), d, 1.0 / math.sqrt(d) if scale is None else scale, at(ov),
-               _ptr(lse if want_lse else None), rows, _ptr(workspace), ws_bytes)
-    _check(st, "losa_packed_attn_fwd")
+        _arg(workspace, "workspace", dev, nbytes=need)
+        ws_at, ws_bytes = workspace.data_ptr(), workspace.nbytes
+    st = _call(dev, lib.losa_packed_attn_fwd, qv, kv, vv, rows, k_rows, plan._at,
+               plan.data.data_ptr(), d, 1.0 / math.sqrt(d) if scale is None else scale, ov, lse_at,
+               rows, ws_at, ws_bytes)
+    if st:
+        _check(st, "losa_packed_attn_fwd")
     return (out, lse) if want_lse else out
 
 

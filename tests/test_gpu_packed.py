@@ -378,7 +378,7 @@ def test_device_argument_checks(L):
         (lambda: L.losa_packed_attn_fwd(q[:, :2], k, k, p), ValueError, "q must have shape"),
         (lambda: L.losa_packed_attn_fwd(q, k[:, :1], k, p), ValueError, "k must have shape"),
         (lambda: L.losa_packed_attn_fwd(q, k, k[:, :, :32], p), ValueError, "v must have shape"),
-        (lambda: L.losa_packed_attn_fwd(q, k, k[:499], p), ValueError, "k has 500 rows"),
+        (lambda: L.losa_packed_attn_fwd(q, k, k[:499], p), ValueError, "v must have shape"),
         (lambda: L.losa_packed_attn_fwd(q, k[:499], k[:499], p), L.LosaError, "INVALID_SHAPE"),
         (lambda: L.losa_packed_attn_fwd(q[:9], k, k, p), L.LosaError, "INVALID_SHAPE"),
         (lambda: L.losa_packed_attn_fwd(q, k, k, p, out=q[:9].clone()), ValueError, "out must have"),

@@ -131,8 +131,13 @@ def test_plan_argument_checks(L):
     assert call(plan=at, room=64) == 0
 
 
+class View(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64),
+                ("head", ctypes.c_int64)]
+
+
 def view(L, data=FAKE, token=512, head=128):
-    return L._View(data, 0, token, head)
+    return View(data, 0, token, head)
 
 
 def fwd(L, q=1, k=1, v=1, o=1, q_rows=40, k_rows=4000, plan=FAKE, d=128, scale=0.1, lse=None,

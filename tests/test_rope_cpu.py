@@ -53,16 +53,44 @@ def test_table_capacity(L):
     assert L.lib.losa_rope_table(1, one(1 << 10), one(1 << 21), 1e4, room, 1 << 40) == 2
 
 
+class View(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64),
+                ("head", ctypes.c_int64)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int), ("axis_dim", ctypes.c_int * 4),
+                ("axis_len", ctypes.c_int * 4), ("table", ctypes.c_void_p),
+                ("pos", ctypes.c_void_p), ("pos_batch", ctypes.c_int64), ("pairs", ctypes.c_int)]
+
+
+class QkNorm(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int), ("all_heads", ctypes.c_int), ("eps", ctypes.c_float),
+                ("q_weight", ctypes.c_void_p), ("q_bias", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p), ("k_bias", ctypes.c_void_p)]
+
+
+def test_structures_are_packed_as_c_lays_them_out(L):
+    """The binding passes structures as bytes: the layout a C compiler gives them."""
+    ints = ctypes.c_int * 4
+    assert bytes(View(1 << 40, 2, 3, 4)) == L._VIEW(1 << 40, 2, 3, 4)
+    t = L.RopeTable(None, (4, 6), (7, 8))
+    assert bytes(Rotation(2, ints(4, 6), ints(7, 8), 1 << 33, 1 << 34, 9, 1)) == \
+        t._head + L._ROTATION(1 << 33, 1 << 34, 9, 1)
+    assert bytes(QkNorm(2, 1, 0.5, 1 << 33, None, 8, 1 << 50)) == \
+        L._QK_NORM(2, True, 0.5, 1 << 33, 0, 8, 1 << 50)
+
+
 def rotation(L, **kw):
     a = dict(n_axes=3, dim=(44, 42, 42, 0), len=(21, 30, 52, 0), table=FAKE, pos=FAKE, pos_batch=0,
              pairs=0)
     a.update(kw)
-    return L._Rotation(a["n_axes"], (ctypes.c_int * 4)(*a["dim"]), (ctypes.c_int * 4)(*a["len"]),
+    return Rotation(a["n_axes"], (ctypes.c_int * 4)(*a["dim"]), (ctypes.c_int * 4)(*a["len"]),
                        a["table"], a["pos"], a["pos_batch"], a["pairs"])
 
 
 def view(L, data=FAKE, batch=100 * 512, token=512, head=128):
-    return L._View(data, batch, token, head)
+    return View(data, batch, token, head)
 
 
 def rope(L, x=None, y=None, rot=None, dtype=1, B=2, N=100, N_pad=100, H=4, d=128, **kw):
@@ -101,7 +129,7 @@ def test_overlapping_output_rows_are_refused(L, kw):
 
 
 def norms(L, kind=1, all_heads=0, eps=1e-6, qw=None, qb=None, kw=None, kb=None):
-    return L._QkNorm(kind, all_heads, eps, qw, qb, kw, kb)
+    return QkNorm(kind, all_heads, eps, qw, qb, kw, kb)
 
 
 def qkn(L, q=1, k=1, v=1, qo=1, ko=1, vo=1, norm=None, rot=1, dtype=1, H=4, Hkv=2, d=128, N_pad=100):
