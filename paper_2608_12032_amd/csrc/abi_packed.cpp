@@ -177,6 +177,8 @@ losa_status losa_packed_attn_fwd(const losa_view* q, const losa_view* k, const l
   a.H_kv = info->H_kv;
   a.G = info->H / info->H_kv;
   a.causal = info->causal;
+  a.by_G = losa::fast_div((uint32_t)a.G);
+  a.by_H_kv = losa::fast_div((uint32_t)a.H_kv);
   a.n_tiles = info->n_tiles;
   a.tile_rows = info->tile_rows;
   a.scale_log2 = scale * 1.4426950408889634f;

@@ -23,6 +23,22 @@ struct PackedJoin {
   int64_t q_row;  // row of q
   int32_t in_group, part, step, n;
 };
+// Division by a number of the call, n / d for any 32-bit n: a product and two shifts
+// (Granlund and Montgomery, "Division by Invariant Integers using Multiplication").
+struct FastDiv {
+  uint32_t d, m, s1, s2;
+};
+inline FastDiv fast_div(uint32_t d) {
+  uint32_t l = 0;
+  while (((uint64_t)1 << l) < d) ++l;
+  return {d, (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << l) - d)) / d + 1), l < 1 ? l : 1,
+          l < 1 ? 0 : l - 1};
+}
+__device__ __forceinline__ int divide(int n, const FastDiv& f) {
+  const uint32_t t = __umulhi(f.m, (uint32_t)n);
+  return (int)((t + (((uint32_t)n - t) >> f.s1)) >> f.s2);
+}
+
 struct PackedArgs {
   const PackedItem* items;
   const PackedJoin* joins;
@@ -34,6 +50,7 @@ struct PackedArgs {
   int64_t lse_head;
   int64_t q_rows, k_rows;
   int H_kv, G, causal;
+  FastDiv by_G, by_H_kv;
   int n_tiles;  // items below this are tiles, the others parts of few-row sequences
   int tile_rows;
   float scale_log2;

@@ -91,14 +91,14 @@ struct Extent {
   int shift;  // causal: token i sees keys up to i + shift
 };
 template <int BLK>
-__device__ __forceinline__ Extent extent(const PackedItem& it, int G, int causal) {
+__device__ __forceinline__ Extent extent(const PackedItem& it, const PackedArgs& a) {
   Extent x;
   x.shift = it.k_len - it.q_len;
-  int last = (it.row0 + BLK - 1) / G;
+  int last = divide(it.row0 + BLK - 1, a.by_G);
   last = last < it.q_len ? last : it.q_len - 1;
-  const int top = causal && last + x.shift + 1 < it.c1 ? last + x.shift + 1 : it.c1;
+  const int top = a.causal && last + x.shift + 1 < it.c1 ? last + x.shift + 1 : it.c1;
   x.n = top > it.c0 ? top - it.c0 : 0;
-  x.seen0 = causal ? it.row0 / G + x.shift + 1 - it.c0 : x.n;
+  x.seen0 = a.causal ? divide(it.row0, a.by_G) + x.shift + 1 - it.c0 : x.n;
   return x;
 }
 
@@ -114,7 +114,7 @@ template <int D>
 __device__ __forceinline__ Row<D> row_of(const PackedArgs& a, const PackedItem& it, const Extent& x,
                                          int kvh, int row, int g) {
   Row<D> r;
-  const int tok = row / a.G;
+  const int tok = divide(row, a.by_G);
   r.valid = tok < it.q_len;
   r.left = x.n;
   if (a.causal && r.valid && tok + x.shift + 1 - it.c0 < x.n) r.left = tok + x.shift + 1 - it.c0;
@@ -247,7 +247,7 @@ __device__ __forceinline__ bool not_finite(const f32x16_t* oacc, bool counts) {
 
 // Unit of this workgroup: (unit, key head), the heads of a unit side by side.
 __device__ __forceinline__ PackedItem unit_of(const PackedArgs& a, int* kvh) {
-  const int unit = (int)blockIdx.x / a.H_kv;
+  const int unit = divide((int)blockIdx.x, a.by_H_kv);
   *kvh = (int)blockIdx.x - unit * a.H_kv;
   return a.items[unit];
 }
@@ -268,7 +268,7 @@ struct RowOut {
   int64_t at, lse;
 };
 __device__ __forceinline__ RowOut row_out(const PackedArgs& a, const PackedItem& it, int kvh, int row) {
-  const int tok = row / a.G;
+  const int tok = divide(row, a.by_G);
   const int64_t head = kvh * a.G + (row - tok * a.G);
   if (tok >= it.q_len) return {-1, 0};
   return {(it.q0 + tok) * a.ot + head * a.oh, head * a.lse_head + it.q0 + tok};
@@ -312,7 +312,7 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
     int kvh;
     const PackedItem it = unit_of(a, &kvh);
     if (!inside(a, it)) return;
-    const Extent x = extent<BLK>(it, a.G, a.causal);
+    const Extent x = extent<BLK>(it, a);
     const int n = x.n;
     hidden = n - x.seen0;
     const int S = ((n + 31) / 32 + 1) & ~1;  // sub-tiles, a multiple of the loop's half
@@ -441,7 +441,7 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
       const PackedArgs b = late_args();
       int kvh;
       const PackedItem it = unit_of(b, &kvh);
-      const Extent x = extent<BLK>(it, b.G, b.causal);
+      const Extent x = extent<BLK>(it, b);
       const Row<D> row = row_of<D>(b, it, x, kvh, it.row0 + w * 32 + er, eg);
       const int whole = wave_min(row.left);
       const uint32_t ks = (uint32_t)b.kt * 2, vs = (uint32_t)b.vt * 2;
@@ -471,6 +471,7 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
     }
   }
 
+  const PackedArgs b = late_args();
   const float l_tot = add_partner(l_run);
   const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
   // O leaves through this wave's part of the K ring, which no wave reads any more, so
@@ -489,7 +490,6 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
     }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
-  const PackedArgs b = late_args();
 #pragma unroll
   for (int z = 0; z < C::SUB; z += 1024) {
     const int r = (z + el * 16) / C::KROW, c = (el * 16 % C::KROW) >> 4;
@@ -524,7 +524,7 @@ __device__ __forceinline__ void few_unit(const PackedArgs& a, PackedLds<D>& lds)
   int kvh;
   const PackedItem it = unit_of(a, &kvh);
   if (!inside(a, it)) return;
-  const Extent x = extent<32>(it, a.G, a.causal);
+  const Extent x = extent<32>(it, a);
   const int n = x.n;
   const char* kb = first_key(a.k, it, a.kt, a.kh, kvh);
   const char* vb = first_key(a.v, it, a.vt, a.vh, kvh);
@@ -697,7 +697,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(const PackedArgs 
   constexpr int PL = D / 64;  // values per lane
   __shared__ float ml[kJoinWaves][2];
   __shared__ float opart[kJoinWaves][D];
-  const int unit = (int)blockIdx.x / a.H_kv;
+  const int unit = divide((int)blockIdx.x, a.by_H_kv);
   const int kvh = (int)blockIdx.x - unit * a.H_kv;
   const PackedJoin j = a.joins[unit];
   const int lane = threadIdx.x & 63;

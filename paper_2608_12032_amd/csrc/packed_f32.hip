@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
   const int lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lm = lane % M, g = lane / M;
-  const int unit = (int)blockIdx.x / a.H_kv;
+  const int unit = divide((int)blockIdx.x, a.by_H_kv);
   const int kvh = (int)blockIdx.x - unit * a.H_kv;
   const PackedItem it = a.items[unit];
   // (a plan's units lie inside q and k; nothing is read or written for one that does not)
@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
     return;
   const int G = a.G;
   const int shift = it.k_len - it.q_len;  // causal: token i sees keys <= i + shift
-  int last = (it.row0 + ROWS - 1) / G;
+  int last = divide(it.row0 + ROWS - 1, a.by_G);
   last = last < it.q_len ? last : it.q_len - 1;
   const int top = a.causal && last + shift + 1 < it.c1 ? last + shift + 1 : it.c1;
   const int n = top > it.c0 ? top - it.c0 : 0;  // keys that some row sees, from c0 on
@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
 #pragma unroll
   for (int rg = 0; rg < RG; ++rg) {
     const int row = it.row0 + rg * M + lm;
-    const int tok = row / G;
+    const int tok = divide(row, a.by_G);
     valid[rg] = tok < it.q_len;
     left[rg] = n;
     if (a.causal && valid[rg] && tok + shift + 1 - it.c0 < n) left[rg] = tok + shift + 1 - it.c0;
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
     }
   }
   if (a.causal) {
-    const int first = it.row0 / G + shift + 1 - it.c0;  // (the first row's)
+    const int first = divide(it.row0, a.by_G) + shift + 1 - it.c0;  // (the first row's)
     whole = first < n ? first : n;
   }
 
@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
       const int64_t at = (int64_t)(it.part + tid) * a.H_kv + kvh;
       *reinterpret_cast<f32x2_t*>(a.part_ml + 2 * at) = f32x2_t{wgt[kWaves], lf};
     } else if (a.lse != nullptr) {
-      const int row = it.row0 + tid, tok = row / G;
+      const int row = it.row0 + tid, tok = divide(row, a.by_G);
       a.lse[(int64_t)(kvh * G + (row - tok * G)) * a.lse_head + it.q0 + tok] =
           lf == 0.f ? -INFINITY : (wgt[kWaves] + __log2f(lf)) * kLn2;
     }
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
     const float inv = lf == 0.f ? 0.f : 1.0f / lf;
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] *= inv;
-    const int row = it.row0 + r, tok = row / G;
+    const int row = it.row0 + r, tok = divide(row, a.by_G);
     float* const op = static_cast<float*>(a.o) + (it.q0 + tok) * a.ot +
                       (int64_t)(kvh * G + (row - tok * G)) * a.oh;
     *reinterpret_cast<f32x4_t*>(op + d4) = acc;
