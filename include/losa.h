@@ -425,8 +425,8 @@ size_t losa_packed_workspace_bytes(const losa_packed_info* info, int d);
  * O = softmax(scale Q K^T + mask) V of every sequence of the plan.
  *
  * q, k, v     views (batch stride unused) of q_rows x H, k_rows x H_kv rows of d, at
- *             least info->q_rows and info->k_rows of them.  k and v: token stride
- *             >= d, at most 64 MiB.
+ *             least info->q_rows and info->k_rows of them.  q and o: strides below
+ *             2^31 elements; k and v: token stride >= d, at most 64 MiB.
  * plan        device, 8-byte aligned, what losa_packed_plan filled together with `info`.
  * o           out, view like q: the sequences' rows.  A row that sees no key is 0.
  *             Rows that no sequence owns are left as they are.  May be q (same view).

@@ -129,6 +129,8 @@ losa_status losa_packed_attn_fwd(const losa_view* q, const losa_view* k, const l
   losa_view qv, kv[2] = {}, ov;
   if ((st = take_view("q", q, &qv, el, 1, q_rows, info->H, d, false)) != LOSA_OK) return st;
   if ((st = take_view("o", o, &ov, el, 1, q_rows, info->H, d, true)) != LOSA_OK) return st;
+  if (((qv.token | qv.head | ov.token | ov.head) >> 31) != 0)
+    return fail(LOSA_ERR_INVALID_SHAPE, "q and o: strides must be below 2^31 elements");
   if (info->k_rows > 0) {
     for (int i = 0; i < 2; ++i) {
       const char* const name = i == 0 ? "k" : "v";

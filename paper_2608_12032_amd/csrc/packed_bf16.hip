@@ -39,11 +39,12 @@ namespace losa {
 
 namespace {
 
-// Scores of sub-tile keys (this lane's 16) at or beyond `left` -> -inf.
+// Scores of the sub-tile's keys (this lane's 16) at or beyond `left` -> -inf.
 __device__ __forceinline__ void mask_left(f32x16_t& s, int left, int g) {
+  const int lim = left - 4 * g;  // (compared with constants: no register each)
 #pragma unroll
   for (int t = 0; t < 16; ++t)
-    if (((t >> 2) << 3) + (g << 2) + (t & 3) >= left) s[t] = -INFINITY;
+    if (lim <= ((t >> 2) << 3) + (t & 3)) s[t] = -INFINITY;
 }
 
 // Bound on a lane's sum of 16 probabilities before the running max is raised, as in
@@ -102,36 +103,65 @@ __device__ __forceinline__ Extent extent(const PackedItem& it, const PackedArgs&
   return x;
 }
 
-// A lane's row: its query operand, and how many of the unit's keys it sees.  Rows
-// behind the last take Q = 0 and every key, and are not written.
+// Rows of a unit: row r (from 0) is token tok0 + t under head h of the group, (t, h) =
+// divmod(h0 + r, G).  Rows behind the last are the last row once more: they see what it
+// sees and give what it gives.
+struct Rows {
+  int tok0, h0, last;  // last: number of the last row
+};
+__device__ __forceinline__ Rows rows_of(const PackedArgs& a, const PackedItem& it) {
+  Rows r;
+  r.tok0 = divide(it.row0, a.by_G);
+  r.h0 = it.row0 - r.tok0 * a.G;
+  r.last = it.q_len * a.G - 1 - it.row0;
+  return r;
+}
+struct RowAt {
+  uint32_t t, h;
+};
+__device__ __forceinline__ RowAt row_at(const PackedArgs& a, const Rows& rows, int r) {
+  const int x = rows.h0 + (r < rows.last ? r : rows.last);
+  const int t = divide(x, a.by_G);
+  return {(uint32_t)t, (uint32_t)(x - t * a.G)};
+}
+// Element offset of a row in a view (q and o: strides below 2^31, see abi_packed.cpp).
+__device__ __forceinline__ int64_t row_offset(const PackedArgs& a, const PackedItem& it,
+                                              const Rows& rows, const RowAt& at, int kvh,
+                                              int64_t token, int64_t head) {
+  const int64_t base = (it.q0 + rows.tok0) * token + (int64_t)kvh * a.G * head;
+  return base + (int64_t)((uint64_t)at.t * (uint32_t)token + (uint64_t)at.h * (uint32_t)head);
+}
+
+// Keys of the unit that a row of token `tok` sees.
+__device__ __forceinline__ int keys_seen(const PackedArgs& a, const PackedItem& it, const Extent& x,
+                                         int tok) {
+  const int seen = tok + x.shift + 1 - it.c0;
+  return a.causal && seen < x.n ? seen : x.n;
+}
+// Keys that every row from r on sees (rows see no fewer than those before them).
+__device__ __forceinline__ int seen_from(const PackedArgs& a, const PackedItem& it, const Extent& x,
+                                         const Rows& rows, int r) {
+  const int y = rows.h0 + (r < rows.last ? r : rows.last);
+  return keys_seen(a, it, x, rows.tok0 + divide(y, a.by_G));
+}
+
+// A lane's row: its query operand, and how many of the unit's keys it sees.
 template <int D>
 struct Row {
   bf16x8_t q[D / 16];
   int left;
-  bool valid;
 };
 template <int D>
 __device__ __forceinline__ Row<D> row_of(const PackedArgs& a, const PackedItem& it, const Extent& x,
-                                         int kvh, int row, int g) {
+                                         const Rows& rows, const RowAt& at, int kvh, int g) {
   Row<D> r;
-  const int tok = divide(row, a.by_G);
-  r.valid = tok < it.q_len;
-  r.left = x.n;
-  if (a.causal && r.valid && tok + x.shift + 1 - it.c0 < x.n) r.left = tok + x.shift + 1 - it.c0;
-  const int head = kvh * a.G + (r.valid ? row - tok * a.G : 0);
-  const __bf16* qp = static_cast<const __bf16*>(a.q) + (it.q0 + (r.valid ? tok : 0)) * a.qt +
-                     (int64_t)head * a.qh;
+  r.left = keys_seen(a, it, x, rows.tok0 + (int)at.t);
+  const __bf16* qp = static_cast<const __bf16*>(a.q) +
+                     row_offset(a, it, rows, at, kvh, a.qt, a.qh) + 8 * g;
 #pragma unroll
   for (int st = 0; st < D / 16; ++st)
-    r.q[st] = r.valid ? *reinterpret_cast<const bf16x8_t*>(qp + 16 * st + 8 * g) : bf16x8_t{};
+    r.q[st] = *reinterpret_cast<const bf16x8_t*>(qp + 16 * st);
   return r;
-}
-
-// Keys seen by every row of the wave.
-__device__ __forceinline__ int wave_min(int x) {
-#pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) x = min(x, __shfl_xor(x, o));
-  return __builtin_amdgcn_readfirstlane(x);
 }
 
 // Per-lane global offsets, inside a sub-tile, of the direct load that fills bytes
@@ -234,15 +264,15 @@ __device__ __forceinline__ void slow_sub(uint32_t kbase, const char* vptr, uint3
   }
 }
 
-// Whether a result holds a value that is not finite, in a row that counts.
+// Whether a result holds a value that is not finite.
 template <int DB>
-__device__ __forceinline__ bool not_finite(const f32x16_t* oacc, bool counts) {
+__device__ __forceinline__ bool not_finite(const f32x16_t* oacc) {
   float bad = 0.f;  // becomes NaN
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int t = 0; t < 16; ++t) bad = __builtin_fmaf(oacc[db][t], 0.f, bad);
-  return __ballot(counts && bad != 0.f) != 0;
+  return __ballot(bad != 0.f) != 0;
 }
 
 // Unit of this workgroup: (unit, key head), the heads of a unit side by side.
@@ -255,7 +285,7 @@ __device__ __forceinline__ PackedItem unit_of(const PackedArgs& a, int* kvh) {
 __device__ __forceinline__ bool inside(const PackedArgs& a, const PackedItem& it) {
   return it.q0 >= 0 && it.q_len >= 0 && it.q0 + it.q_len <= a.q_rows && it.k0 >= 0 &&
          it.k_len >= 0 && it.k0 + it.k_len <= a.k_rows && it.c0 >= 0 && it.c1 <= it.k_len &&
-         it.row0 >= 0;
+         it.row0 >= 0 && it.row0 < (int64_t)it.q_len * a.G;
 }
 __device__ __forceinline__ const char* first_key(const void* x, const PackedItem& it, int64_t token,
                                                  int64_t head, int kvh) {
@@ -263,15 +293,18 @@ __device__ __forceinline__ const char* first_key(const void* x, const PackedItem
                                        kvh * head);
 }
 
-// Where a row's output goes (elements from o and from lse); at < 0: nowhere.
+// Where a row's output goes: bytes from o, elements from lse.
 struct RowOut {
   int64_t at, lse;
 };
-__device__ __forceinline__ RowOut row_out(const PackedArgs& a, const PackedItem& it, int kvh, int row) {
-  const int tok = divide(row, a.by_G);
-  const int64_t head = kvh * a.G + (row - tok * a.G);
-  if (tok >= it.q_len) return {-1, 0};
-  return {(it.q0 + tok) * a.ot + head * a.oh, head * a.lse_head + it.q0 + tok};
+__device__ __forceinline__ RowOut row_out(const PackedArgs& a, const PackedItem& it, const Rows& rows,
+                                          const RowAt& at, int kvh) {
+  RowOut r;
+  r.at = 2 * row_offset(a, it, rows, at, kvh, a.ot, a.oh);
+  r.lse = 0;
+  if (a.lse != nullptr)
+    r.lse = (int64_t)(kvh * a.G + (int)at.h) * a.lse_head + it.q0 + rows.tok0 + at.t;
+  return r;
 }
 
 constexpr int NW = 4;  // waves of a workgroup
@@ -306,6 +339,7 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
   float m_run = kNegBig;  // max used for exp2 (log2 units)
   float l_run = 0.f;      // this lane's share of the row sum
   int hidden;             // keys of the unit that some row does not see, if > 0
+  int used;               // rows of the sequence from this wave's first on
   {
     const int lane = threadIdx.x & 63;
     const int g = lane >> 5;
@@ -340,10 +374,13 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
         }
       }
     }
-    const Row<D> row = row_of<D>(a, it, x, kvh, it.row0 + w * 32 + (lane & 31), g);
-    if (g == 0) out[w * 32 + lane] = row_out(a, it, kvh, it.row0 + w * 32 + lane);
+    const Rows rows = rows_of(a, it);
+    const RowAt at = row_at(a, rows, w * 32 + (lane & 31));
+    const Row<D> row = row_of<D>(a, it, x, rows, at, kvh, g);
+    if (g == 0) out[w * 32 + lane] = row_out(a, it, rows, at, kvh);
+    used = rows.last + 1 - w * 32;
     const int left = row.left;
-    const int whole = wave_min(left);
+    const int whole = seen_from(a, it, x, rows, w * 32);  // keys every row of the wave sees
     uint32_t ka[C::KS], va = v_operand<D>(lds0 + C::RING, lane);
 #pragma unroll
     for (int st = 0; st < C::KS; ++st) ka[st] = k_operand<D>(lds0, lane, st);
@@ -359,6 +396,9 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
         for (int st = 0; st < 2; ++st) pb[a2][st] = bf16x8_t{};
       wait_vm_barrier<0>();
       mfma_pair<D, BLK, BK, true, false>(ka, 0, row.q, sc[0], va, 0, pb[1], oacc);
+      // the first reference is the first sub-tile's max
+      if (whole < 32) mask_left(sc[0], left, g);
+      m_run = fmaxf(m_run, sub_max(sc[0]) * scale_log2);
 
       // sub-iteration s = R u + H of the block-sparse forward: scores of s + 1, softmax
       // of s, P V of s - 1; K slot H takes sub-tile s + R, V slot (H + R - 2) % R sub-tile
@@ -430,7 +470,7 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
   const int er = el & 31, eg = el >> 5;
   if (hidden > 0) {
     // some row does not see some key of the unit: has a value that is not finite spread?
-    const bool mine = not_finite<C::DB>(oacc, out[w * 32 + er].at >= 0);
+    const bool mine = not_finite<C::DB>(oacc);
     int* const flag = reinterpret_cast<int*>(smem + C::RING);  // (no output passes there)
     if (el == 0) flag[w] = mine;
     __syncthreads();
@@ -442,8 +482,9 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
       int kvh;
       const PackedItem it = unit_of(b, &kvh);
       const Extent x = extent<BLK>(it, b);
-      const Row<D> row = row_of<D>(b, it, x, kvh, it.row0 + w * 32 + er, eg);
-      const int whole = wave_min(row.left);
+      const Rows rows = rows_of(b, it);
+      const Row<D> row = row_of<D>(b, it, x, rows, row_at(b, rows, w * 32 + er), kvh, eg);
+      const int whole = seen_from(b, it, x, rows, w * 32);
       const uint32_t ks = (uint32_t)b.kt * 2, vs = (uint32_t)b.vt * 2;
 #pragma unroll
       for (int db = 0; db < C::DB; ++db) oacc[db] = f32x16_t{};
@@ -490,15 +531,23 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
     }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
-#pragma unroll
-  for (int z = 0; z < C::SUB; z += 1024) {
+  // (a whole tile's stores are not tested, and a ragged one's last row is written once)
+  const RowOut* const ro = out + w * 32 + el * 16 / C::KROW;
+  char* const ob = static_cast<char*>(b.o) + (el * 16 % C::KROW);
+  auto store = [&](int z) {
     const int r = (z + el * 16) / C::KROW, c = (el * 16 % C::KROW) >> 4;
-    const int64_t at = out[w * 32 + r].at;
-    if (at >= 0)
-      *reinterpret_cast<f32x4_t*>(static_cast<__bf16*>(b.o) + at + 8 * c) =
-          *reinterpret_cast<const f32x4_t*>(ot + r * C::KROW + (kswz<D, BLK, BK>(r, c) << 4));
+    *reinterpret_cast<f32x4_t*>(ob + ro[z / C::KROW].at) = *reinterpret_cast<const f32x4_t*>(
+        ot + r * C::KROW + (kswz<D, BLK, BK>(r, c) << 4));
+  };
+  if (used >= 32) {
+#pragma unroll
+    for (int z = 0; z < C::SUB; z += 1024) store(z);
+  } else {
+#pragma unroll
+    for (int z = 0; z < C::SUB; z += 1024)
+      if ((z + el * 16) / C::KROW < used) store(z);
   }
-  if (b.lse != nullptr && eg == 0 && out[w * 32 + er].at >= 0)
+  if (b.lse != nullptr && eg == 0 && er < used)
     b.lse[out[w * 32 + er].lse] = l_tot == 0.f ? -INFINITY : (m_run + __log2f(l_tot)) * kLn2;
 }
 
@@ -551,12 +600,14 @@ __device__ __forceinline__ void few_unit(const PackedArgs& a, PackedLds<D>& lds)
     load_k(w);
     load_v(w);
   }
-  Row<D> row = row_of<D>(a, it, x, kvh, it.row0 + r32, g);
+  const Rows unit_rows = rows_of(a, it);
+  const RowAt row_in = row_at(a, unit_rows, r32);
+  Row<D> row = row_of<D>(a, it, x, unit_rows, row_in, kvh, g);
   // (waited for here, not inside the loop, where the wait would cover the loads in flight)
 #pragma unroll
   for (int st = 0; st < C::KS; ++st) asm volatile("" : "+v"(row.q[st]));
-  if (w == 0 && g == 0) out[lane] = row_out(a, it, kvh, it.row0 + lane);
-  const int whole = wave_min(row.left);
+  if (w == 0 && g == 0) out[lane] = row_out(a, it, unit_rows, row_in, kvh);
+  const int whole = seen_from(a, it, x, unit_rows, 0);
   f32x16_t oacc[C::DB];
 #pragma unroll
   for (int db = 0; db < C::DB; ++db) oacc[db] = f32x16_t{};
@@ -592,7 +643,7 @@ __device__ __forceinline__ void few_unit(const PackedArgs& a, PackedLds<D>& lds)
     load_v(s + NW);
   }
   wait_vm<0>();
-  if (n > x.seen0 && not_finite<C::DB>(oacc, r32 < it.q_len * a.G - it.row0)) {
+  if (n > x.seen0 && not_finite<C::DB>(oacc)) {
     // some row does not see some key: this wave's sub-tiles again, see slow_sub
 #pragma unroll
     for (int db = 0; db < C::DB; ++db) oacc[db] = f32x16_t{};
@@ -612,7 +663,7 @@ __device__ __forceinline__ void few_unit(const PackedArgs& a, PackedLds<D>& lds)
   // the waves' states through LDS: O of wave w, [row][d] in 16-byte chunks swizzled by
   // row, over its own slots
   const float l_tot = add_partner(l_run);
-  const int rows = it.q_len * a.G - it.row0;
+  const int rows = unit_rows.last + 1;
   constexpr int CH = D / 4;  // chunks of a row
   auto chunk = [&](int wave, int r, int c) {
     return reinterpret_cast<f32x4_t*>(smem + wave * 2 * C::SUB + (r * CH + (c ^ (r % CH))) * 16);
@@ -652,11 +703,11 @@ __device__ __forceinline__ void few_unit(const PackedArgs& a, PackedLds<D>& lds)
       const int64_t at = (int64_t)(it.part + r) * a.H_kv + kvh;
       *reinterpret_cast<f32x4_t*>(a.part_o + at * D + 4 * c) = acc;
       if (c == 0) *reinterpret_cast<f32x2_t*>(a.part_ml + 2 * at) = f32x2_t{m, l};
-    } else if (out[r].at >= 0) {
+    } else {
       const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] *= inv;
-      *reinterpret_cast<bf16x4_t*>(static_cast<__bf16*>(a.o) + out[r].at + 4 * c) =
+      *reinterpret_cast<bf16x4_t*>(static_cast<char*>(a.o) + out[r].at + 8 * c) =
           __builtin_convertvector(acc, bf16x4_t);
       if (a.lse != nullptr && c == 0)
         a.lse[out[r].lse] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
