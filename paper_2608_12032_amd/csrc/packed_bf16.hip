@@ -53,15 +53,25 @@ constexpr float kSumBound = 1048576.0f;
 
 __device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < INFINITY; }
 
-// Buffer resource of sub-tile x (32 rows of D elements, `stride` bytes apart) of a
-// range of n rows at base: rows at or beyond n read as 0.
+// The sub-tiles of 32 rows of D elements, `stride` bytes apart, of a range of rows, one
+// after another.  Each has a buffer resource of its own, so that rows behind the end read
+// as 0 and no offset passes 32 bits.
 template <int D>
-__device__ __forceinline__ i32x4_t sub_rsrc(const char* base, uint32_t stride, int x, int n) {
-  int left = n - 32 * x;
-  left = left < 0 ? 0 : (left > 32 ? 32 : left);
-  return rsrc_words(base + (int64_t)x * 32 * stride,
-                    left == 0 ? 0u : (uint32_t)(left - 1) * stride + 2 * D);
-}
+struct Stream {
+  const char* at;  // the next sub-tile
+  int left;        // rows from it on
+  uint32_t stride;
+
+  __device__ __forceinline__ Stream(const char* base, int n, uint32_t st, int first)
+      : at(base + (int64_t)first * 32 * st), left(n - 32 * first), stride(st) {}
+  __device__ __forceinline__ i32x4_t next() {
+    const int rows = left > 32 ? 32 : left;
+    const i32x4_t rs = rsrc_words(at, rows <= 0 ? 0u : (uint32_t)(rows - 1) * stride + 2 * D);
+    at += (uint64_t)stride * 32;
+    left -= 32;
+    return rs;
+  }
+};
 
 // The call's arguments, read again from where the launch put them.  After the loop a
 // kernel takes what it needs from here, so that the loop carries none of it.
@@ -83,7 +93,10 @@ __device__ __forceinline__ int late_lane() {
 
 // The scalar registers of a buffer resource are written: five wait states until a load
 // may read them, which the compiler does not count for loads in inline assembly.
-__device__ __forceinline__ void settle(i32x4_t& rs) { asm volatile("s_nop 4" : "+s"(rs)); }
+__device__ __forceinline__ void settle(i32x4_t& a) { asm volatile("s_nop 4" : "+s"(a)); }
+__device__ __forceinline__ void settle(i32x4_t& a, i32x4_t& b) {
+  asm volatile("s_nop 4" : "+s"(a), "+s"(b));
+}
 
 // A unit as its rows see it: keys that count, relative to c0.
 struct Extent {
@@ -361,11 +374,11 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
       voffs[u] = v_offset<D>((w * C::LPW + u) * 1024 + lane * 16, vs);
     }
     if (S > 0) {
+      Stream<D> kf(kb, n, ks, 0), vf(vb, n, vs, 0);
 #pragma unroll
       for (int y = 0; y < R; ++y) {
-        i32x4_t krs = sub_rsrc<D>(kb, ks, y, n), vrs = sub_rsrc<D>(vb, vs, y, n);
-        settle(krs);
-        settle(vrs);
+        i32x4_t krs = kf.next(), vrs = vf.next();
+        settle(krs, vrs);
 #pragma unroll
         for (int u = 0; u < C::LPW; ++u) {
           dma16(lds0 + y * C::SUB + (w * C::LPW + u) * 1024, krs, koffs[u], 0);
@@ -403,6 +416,7 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
       // sub-iteration s = R u + H of the block-sparse forward: scores of s + 1, softmax
       // of s, P V of s - 1; K slot H takes sub-tile s + R, V slot (H + R - 2) % R sub-tile
       // s + R - 2 (behind the end of the keys: zeros)
+      Stream<D> kf(kb, n, ks, R), vf(vb, n, vs, R - 2);
       auto sub_iter = [&](auto hh, int u) {
         constexpr int H = decltype(hh)::value;
         const int s = R * u + H;
@@ -414,10 +428,8 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
         // (opaque, so that the loads' LDS addresses are not kept in a register each)
         uint32_t ring = lds0 + w * C::LPW * 1024;
         asm volatile("" : "+s"(ring));
-        i32x4_t krs = sub_rsrc<D>(kb, ks, s + R, n);
-        i32x4_t vrs = sub_rsrc<D>(vb, vs, s + R - 2, n);
-        settle(krs);
-        settle(vrs);
+        i32x4_t krs = kf.next(), vrs = vf.next();
+        settle(krs, vrs);
         wait_vm_barrier<(R - 2) * 2 * C::LPW>();
         auto issue = [&](int t) {
           if (t < C::LPW) {
@@ -492,11 +504,11 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
       l_run = 0.f;
       __bf16* const pw = reinterpret_cast<__bf16*>(smem + C::SUB) + w * 32 * 32;
       static_assert(C::SUB + NW * 2048 <= C::RING, "the probabilities fit behind K slot 0");
+      Stream<D> kf(first_key(b.k, it, b.kt, b.kh, kvh), x.n, ks, 0);
+      Stream<D> vf(first_key(b.v, it, b.vt, b.vh, kvh), x.n, vs, 0);
       for (int s = 0; 32 * s < x.n; ++s) {
-        i32x4_t krs = sub_rsrc<D>(first_key(b.k, it, b.kt, b.kh, kvh), ks, s, x.n);
-        i32x4_t vrs = sub_rsrc<D>(first_key(b.v, it, b.vt, b.vh, kvh), vs, s, x.n);
-        settle(krs);
-        settle(vrs);
+        i32x4_t krs = kf.next(), vrs = vf.next();
+        settle(krs, vrs);
         lds_read_barrier();
 #pragma unroll 1
         for (int u = 0; u < C::LPW; ++u) {
@@ -585,13 +597,13 @@ __device__ __forceinline__ void few_unit(const PackedArgs& a, PackedLds<D>& lds)
     voffs[u] = v_offset<D>(u * 1024 + lane * 16, vs);
   }
   auto load_k = [&](int s) {
-    i32x4_t rs = sub_rsrc<D>(kb, ks, s, n);
+    i32x4_t rs = Stream<D>(kb, n, ks, s).next();
     settle(rs);
 #pragma unroll
     for (int u = 0; u < LD; ++u) dma16(lds0 + u * 1024, rs, koffs[u], 0);
   };
   auto load_v = [&](int s) {
-    i32x4_t rs = sub_rsrc<D>(vb, vs, s, n);
+    i32x4_t rs = Stream<D>(vb, n, vs, s).next();
     settle(rs);
 #pragma unroll
     for (int u = 0; u < LD; ++u) dma16(lds0 + C::SUB + u * 1024, rs, voffs[u], 0);

@@ -170,6 +170,9 @@ def test_forward_view_refusals(L, which, kw, code):
 
 def test_forward_stride_refusals(L):
     assert fwd(L, o=view(L, token=64)) == 2 and fwd(L, o=view(L, head=0)) == 2
+    for which in "qo":  # row offsets are products of 32-bit numbers
+        assert fwd(L, **{which: view(L, head=1 << 31)}) == 2
+        assert fwd(L, **{which: view(L, token=1 << 31)}) == 2
     for which in "kv":
         assert fwd(L, **{which: view(L, token=64)}) == 2
         assert fwd(L, **{which: view(L, token=(1 << 25) + 8)}) == 2
