@@ -178,7 +178,6 @@ losa_status losa_packed_attn_fwd(const losa_view* q, const losa_view* k, const l
   a.k_rows = k_rows;
   a.H_kv = info->H_kv;
   a.G = info->H / info->H_kv;
-  a.causal = info->causal;
   a.by_G = losa::fast_div((uint32_t)a.G);
   a.by_H_kv = losa::fast_div((uint32_t)a.H_kv);
   a.n_tiles = info->n_tiles;

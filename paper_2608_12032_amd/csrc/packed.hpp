@@ -11,13 +11,19 @@ namespace losa {
 // Packed attention (packed_plan.cpp, packed_bf16.hip, packed_f32.hip).  A row of a
 // sequence is one query token under one query head of a key head's group, numbered
 // token * G + head in group, so that rows which share keys fill a tile together.
-// One unit of work: rows row0 .. of a sequence against its keys c0 .. c1.
+// One unit of work: a tile's or part's rows against a range of keys.  Row r (from 0) is
+// token t under head h of the group, (t, h) = divmod(head0 + r, G), and sees the first
+// seen + t of the keys, `keys` at most.
 struct PackedItem {
-  int64_t q0, k0;        // first row of q and of k the sequence owns
-  int32_t q_len, k_len;  // its tokens
-  int32_t row0, c0, c1;
+  int64_t q_row, k_row;  // rows of q and of k of the unit's first token and key
+  int32_t head0;
+  int32_t rows;  // rows of the sequence from the unit's first on
+  int32_t keys;  // keys that some row of the unit sees
+  int32_t seen;  // (kAllSeen: every row sees them all)
   int32_t part;  // first partial row to write, or -1: the result itself
+  int32_t unused;
 };
+constexpr int32_t kAllSeen = 1 << 30;
 // One row whose keys were split: n partial rows at part, part + step, ...
 struct PackedJoin {
   int64_t q_row;  // row of q
@@ -49,12 +55,20 @@ struct PackedArgs {
   int64_t qt, qh, kt, kh, vt, vh, ot, oh;  // token and head strides, elements
   int64_t lse_head;
   int64_t q_rows, k_rows;
-  int H_kv, G, causal;
+  int H_kv, G;
   FastDiv by_G, by_H_kv;
   int n_tiles;  // items below this are tiles, the others parts of few-row sequences
   int tile_rows;
   float scale_log2;
 };
+// Whether the unit's rows (`tile` at most) and keys lie inside q and k.  (A plan's do;
+// nothing is read or written for one that does not.)
+__device__ __forceinline__ bool inside(const PackedArgs& a, const PackedItem& it, int tile) {
+  const int last = it.head0 + (it.rows < tile ? it.rows : tile) - 1;
+  return (it.q_row >= 0) & (it.k_row >= 0) & (it.head0 >= 0) & (it.rows > 0) & (it.keys >= 0) &
+         (it.q_row + divide(last, a.by_G) < a.q_rows) & (it.k_row + it.keys <= a.k_rows);
+}
+
 // Rows of a tile (fp32: of a wide one; a call of few units takes tiles of 16), rows of
 // a sequence that make it a few-row one.
 constexpr int kPackedTile[2] = {32, 128};  // [bf16]

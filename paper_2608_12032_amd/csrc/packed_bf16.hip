@@ -98,64 +98,30 @@ __device__ __forceinline__ void settle(i32x4_t& a, i32x4_t& b) {
   asm volatile("s_nop 4" : "+s"(a), "+s"(b));
 }
 
-// A unit as its rows see it: keys that count, relative to c0.
-struct Extent {
-  int n;      // keys that some row sees
-  int seen0;  // keys that every row sees
-  int shift;  // causal: token i sees keys up to i + shift
-};
-template <int BLK>
-__device__ __forceinline__ Extent extent(const PackedItem& it, const PackedArgs& a) {
-  Extent x;
-  x.shift = it.k_len - it.q_len;
-  int last = divide(it.row0 + BLK - 1, a.by_G);
-  last = last < it.q_len ? last : it.q_len - 1;
-  const int top = a.causal && last + x.shift + 1 < it.c1 ? last + x.shift + 1 : it.c1;
-  x.n = top > it.c0 ? top - it.c0 : 0;
-  x.seen0 = a.causal ? divide(it.row0, a.by_G) + x.shift + 1 - it.c0 : x.n;
-  return x;
-}
-
-// Rows of a unit: row r (from 0) is token tok0 + t under head h of the group, (t, h) =
-// divmod(h0 + r, G).  Rows behind the last are the last row once more: they see what it
+// Row r of a unit; rows behind the last are the last row once more: they see what it
 // sees and give what it gives.
-struct Rows {
-  int tok0, h0, last;  // last: number of the last row
-};
-__device__ __forceinline__ Rows rows_of(const PackedArgs& a, const PackedItem& it) {
-  Rows r;
-  r.tok0 = divide(it.row0, a.by_G);
-  r.h0 = it.row0 - r.tok0 * a.G;
-  r.last = it.q_len * a.G - 1 - it.row0;
-  return r;
-}
 struct RowAt {
-  uint32_t t, h;
+  uint32_t t, h;  // token from the unit's first on, head in the group
 };
-__device__ __forceinline__ RowAt row_at(const PackedArgs& a, const Rows& rows, int r) {
-  const int x = rows.h0 + (r < rows.last ? r : rows.last);
+__device__ __forceinline__ RowAt row_at(const PackedArgs& a, const PackedItem& it, int r) {
+  const int x = it.head0 + (r < it.rows ? r : it.rows - 1);
   const int t = divide(x, a.by_G);
   return {(uint32_t)t, (uint32_t)(x - t * a.G)};
 }
 // Element offset of a row in a view (q and o: strides below 2^31, see abi_packed.cpp).
 __device__ __forceinline__ int64_t row_offset(const PackedArgs& a, const PackedItem& it,
-                                              const Rows& rows, const RowAt& at, int kvh,
-                                              int64_t token, int64_t head) {
-  const int64_t base = (it.q0 + rows.tok0) * token + (int64_t)kvh * a.G * head;
+                                              const RowAt& at, int kvh, int64_t token, int64_t head) {
+  const int64_t base = it.q_row * token + (int64_t)(kvh * a.G) * head;
   return base + (int64_t)((uint64_t)at.t * (uint32_t)token + (uint64_t)at.h * (uint32_t)head);
 }
-
-// Keys of the unit that a row of token `tok` sees.
-__device__ __forceinline__ int keys_seen(const PackedArgs& a, const PackedItem& it, const Extent& x,
-                                         int tok) {
-  const int seen = tok + x.shift + 1 - it.c0;
-  return a.causal && seen < x.n ? seen : x.n;
+// Keys of the unit that its token t sees.
+__device__ __forceinline__ int keys_seen(const PackedItem& it, int t) {
+  const int seen = it.seen + t;
+  return seen < it.keys ? seen : it.keys;
 }
 // Keys that every row from r on sees (rows see no fewer than those before them).
-__device__ __forceinline__ int seen_from(const PackedArgs& a, const PackedItem& it, const Extent& x,
-                                         const Rows& rows, int r) {
-  const int y = rows.h0 + (r < rows.last ? r : rows.last);
-  return keys_seen(a, it, x, rows.tok0 + divide(y, a.by_G));
+__device__ __forceinline__ int seen_from(const PackedArgs& a, const PackedItem& it, int r) {
+  return keys_seen(it, divide(it.head0 + (r < it.rows ? r : it.rows - 1), a.by_G));
 }
 
 // A lane's row: its query operand, and how many of the unit's keys it sees.
@@ -165,12 +131,11 @@ struct Row {
   int left;
 };
 template <int D>
-__device__ __forceinline__ Row<D> row_of(const PackedArgs& a, const PackedItem& it, const Extent& x,
-                                         const Rows& rows, const RowAt& at, int kvh, int g) {
+__device__ __forceinline__ Row<D> row_of(const PackedArgs& a, const PackedItem& it, const RowAt& at,
+                                         int kvh, int g) {
   Row<D> r;
-  r.left = keys_seen(a, it, x, rows.tok0 + (int)at.t);
-  const __bf16* qp = static_cast<const __bf16*>(a.q) +
-                     row_offset(a, it, rows, at, kvh, a.qt, a.qh) + 8 * g;
+  r.left = keys_seen(it, (int)at.t);
+  const __bf16* qp = static_cast<const __bf16*>(a.q) + row_offset(a, it, at, kvh, a.qt, a.qh) + 8 * g;
 #pragma unroll
   for (int st = 0; st < D / 16; ++st)
     r.q[st] = *reinterpret_cast<const bf16x8_t*>(qp + 16 * st);
@@ -294,15 +259,9 @@ __device__ __forceinline__ PackedItem unit_of(const PackedArgs& a, int* kvh) {
   *kvh = (int)blockIdx.x - unit * a.H_kv;
   return a.items[unit];
 }
-// (A plan's units lie inside q and k; nothing is read or written for one that does not.)
-__device__ __forceinline__ bool inside(const PackedArgs& a, const PackedItem& it) {
-  return it.q0 >= 0 && it.q_len >= 0 && it.q0 + it.q_len <= a.q_rows && it.k0 >= 0 &&
-         it.k_len >= 0 && it.k0 + it.k_len <= a.k_rows && it.c0 >= 0 && it.c1 <= it.k_len &&
-         it.row0 >= 0 && it.row0 < (int64_t)it.q_len * a.G;
-}
 __device__ __forceinline__ const char* first_key(const void* x, const PackedItem& it, int64_t token,
                                                  int64_t head, int kvh) {
-  return reinterpret_cast<const char*>(static_cast<const __bf16*>(x) + (it.k0 + it.c0) * token +
+  return reinterpret_cast<const char*>(static_cast<const __bf16*>(x) + it.k_row * token +
                                        kvh * head);
 }
 
@@ -310,13 +269,12 @@ __device__ __forceinline__ const char* first_key(const void* x, const PackedItem
 struct RowOut {
   int64_t at, lse;
 };
-__device__ __forceinline__ RowOut row_out(const PackedArgs& a, const PackedItem& it, const Rows& rows,
-                                          const RowAt& at, int kvh) {
+__device__ __forceinline__ RowOut row_out(const PackedArgs& a, const PackedItem& it, const RowAt& at,
+                                          int kvh) {
   RowOut r;
-  r.at = 2 * row_offset(a, it, rows, at, kvh, a.ot, a.oh);
+  r.at = 2 * row_offset(a, it, at, kvh, a.ot, a.oh);
   r.lse = 0;
-  if (a.lse != nullptr)
-    r.lse = (int64_t)(kvh * a.G + (int)at.h) * a.lse_head + it.q0 + rows.tok0 + at.t;
+  if (a.lse != nullptr) r.lse = (kvh * a.G + (int64_t)at.h) * a.lse_head + it.q_row + at.t;
   return r;
 }
 
@@ -358,10 +316,9 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
     const int g = lane >> 5;
     int kvh;
     const PackedItem it = unit_of(a, &kvh);
-    if (!inside(a, it)) return;
-    const Extent x = extent<BLK>(it, a);
-    const int n = x.n;
-    hidden = n - x.seen0;
+    if (!inside(a, it, BLK)) return;
+    const int n = it.keys;
+    hidden = n - it.seen;
     const int S = ((n + 31) / 32 + 1) & ~1;  // sub-tiles, a multiple of the loop's half
     const char* kb = first_key(a.k, it, a.kt, a.kh, kvh);
     const char* vb = first_key(a.v, it, a.vt, a.vh, kvh);
@@ -387,13 +344,12 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
         }
       }
     }
-    const Rows rows = rows_of(a, it);
-    const RowAt at = row_at(a, rows, w * 32 + (lane & 31));
-    const Row<D> row = row_of<D>(a, it, x, rows, at, kvh, g);
-    if (g == 0) out[w * 32 + lane] = row_out(a, it, rows, at, kvh);
-    used = rows.last + 1 - w * 32;
+    const RowAt at = row_at(a, it, w * 32 + (lane & 31));
+    const Row<D> row = row_of<D>(a, it, at, kvh, g);
+    if (g == 0) out[w * 32 + lane] = row_out(a, it, at, kvh);
+    used = it.rows - w * 32;
     const int left = row.left;
-    const int whole = seen_from(a, it, x, rows, w * 32);  // keys every row of the wave sees
+    const int whole = seen_from(a, it, w * 32);  // keys every row of the wave sees
     uint32_t ka[C::KS], va = v_operand<D>(lds0 + C::RING, lane);
 #pragma unroll
     for (int st = 0; st < C::KS; ++st) ka[st] = k_operand<D>(lds0, lane, st);
@@ -493,10 +449,8 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
       const PackedArgs b = late_args();
       int kvh;
       const PackedItem it = unit_of(b, &kvh);
-      const Extent x = extent<BLK>(it, b);
-      const Rows rows = rows_of(b, it);
-      const Row<D> row = row_of<D>(b, it, x, rows, row_at(b, rows, w * 32 + er), kvh, eg);
-      const int whole = seen_from(b, it, x, rows, w * 32);
+      const Row<D> row = row_of<D>(b, it, row_at(b, it, w * 32 + er), kvh, eg);
+      const int whole = seen_from(b, it, w * 32);
       const uint32_t ks = (uint32_t)b.kt * 2, vs = (uint32_t)b.vt * 2;
 #pragma unroll
       for (int db = 0; db < C::DB; ++db) oacc[db] = f32x16_t{};
@@ -504,9 +458,9 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
       l_run = 0.f;
       __bf16* const pw = reinterpret_cast<__bf16*>(smem + C::SUB) + w * 32 * 32;
       static_assert(C::SUB + NW * 2048 <= C::RING, "the probabilities fit behind K slot 0");
-      Stream<D> kf(first_key(b.k, it, b.kt, b.kh, kvh), x.n, ks, 0);
-      Stream<D> vf(first_key(b.v, it, b.vt, b.vh, kvh), x.n, vs, 0);
-      for (int s = 0; 32 * s < x.n; ++s) {
+      Stream<D> kf(first_key(b.k, it, b.kt, b.kh, kvh), it.keys, ks, 0);
+      Stream<D> vf(first_key(b.v, it, b.vt, b.vh, kvh), it.keys, vs, 0);
+      for (int s = 0; 32 * s < it.keys; ++s) {
         i32x4_t krs = kf.next(), vrs = vf.next();
         settle(krs, vrs);
         lds_read_barrier();
@@ -584,9 +538,8 @@ __device__ __forceinline__ void few_unit(const PackedArgs& a, PackedLds<D>& lds)
   char* const vptr = smem + w * 2 * C::SUB + C::SUB;
   int kvh;
   const PackedItem it = unit_of(a, &kvh);
-  if (!inside(a, it)) return;
-  const Extent x = extent<32>(it, a);
-  const int n = x.n;
+  if (!inside(a, it, 32)) return;
+  const int n = it.keys;
   const char* kb = first_key(a.k, it, a.kt, a.kh, kvh);
   const char* vb = first_key(a.v, it, a.vt, a.vh, kvh);
   const uint32_t ks = (uint32_t)a.kt * 2, vs = (uint32_t)a.vt * 2;
@@ -612,14 +565,13 @@ __device__ __forceinline__ void few_unit(const PackedArgs& a, PackedLds<D>& lds)
     load_k(w);
     load_v(w);
   }
-  const Rows unit_rows = rows_of(a, it);
-  const RowAt row_in = row_at(a, unit_rows, r32);
-  Row<D> row = row_of<D>(a, it, x, unit_rows, row_in, kvh, g);
+  const RowAt row_in = row_at(a, it, r32);
+  Row<D> row = row_of<D>(a, it, row_in, kvh, g);
   // (waited for here, not inside the loop, where the wait would cover the loads in flight)
 #pragma unroll
   for (int st = 0; st < C::KS; ++st) asm volatile("" : "+v"(row.q[st]));
-  if (w == 0 && g == 0) out[lane] = row_out(a, it, unit_rows, row_in, kvh);
-  const int whole = seen_from(a, it, x, unit_rows, 0);
+  if (w == 0 && g == 0) out[lane] = row_out(a, it, row_in, kvh);
+  const int whole = seen_from(a, it, 0);
   f32x16_t oacc[C::DB];
 #pragma unroll
   for (int db = 0; db < C::DB; ++db) oacc[db] = f32x16_t{};
@@ -655,7 +607,7 @@ __device__ __forceinline__ void few_unit(const PackedArgs& a, PackedLds<D>& lds)
     load_v(s + NW);
   }
   wait_vm<0>();
-  if (n > x.seen0 && not_finite<C::DB>(oacc)) {
+  if (n > it.seen && not_finite<C::DB>(oacc)) {
     // some row does not see some key: this wave's sub-tiles again, see slow_sub
 #pragma unroll
     for (int db = 0; db < C::DB; ++db) oacc[db] = f32x16_t{};
@@ -675,7 +627,7 @@ __device__ __forceinline__ void few_unit(const PackedArgs& a, PackedLds<D>& lds)
   // the waves' states through LDS: O of wave w, [row][d] in 16-byte chunks swizzled by
   // row, over its own slots
   const float l_tot = add_partner(l_run);
-  const int rows = unit_rows.last + 1;
+  const int rows = it.rows;
   constexpr int CH = D / 4;  // chunks of a row
   auto chunk = [&](int wave, int r, int c) {
     return reinterpret_cast<f32x4_t*>(smem + wave * 2 * C::SUB + (r * CH + (c ^ (r % CH))) * 16);

@@ -70,48 +70,35 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
   const int unit = divide((int)blockIdx.x, a.by_H_kv);
   const int kvh = (int)blockIdx.x - unit * a.H_kv;
   const PackedItem it = a.items[unit];
-  // (a plan's units lie inside q and k; nothing is read or written for one that does not)
-  if (it.q0 < 0 || it.q_len < 0 || it.q0 + it.q_len > a.q_rows || it.k0 < 0 || it.k_len < 0 ||
-      it.k0 + it.k_len > a.k_rows || it.c0 < 0 || it.c1 > it.k_len || it.row0 < 0)
-    return;
+  if (!inside(a, it, ROWS)) return;
   const int G = a.G;
-  const int shift = it.k_len - it.q_len;  // causal: token i sees keys <= i + shift
-  int last = divide(it.row0 + ROWS - 1, a.by_G);
-  last = last < it.q_len ? last : it.q_len - 1;
-  const int top = a.causal && last + shift + 1 < it.c1 ? last + shift + 1 : it.c1;
-  const int n = top > it.c0 ? top - it.c0 : 0;  // keys that some row sees, from c0 on
+  const int n = it.keys;
   const int S = (n + CK - 1) / CK;
 
   f32x4_t qr[RG * T::QI];
   int left[RG];  // keys this lane's row of each group sees
   bool valid[RG];
-  int whole = n;  // keys that every row of the unit sees
+  const int whole = it.seen < n ? it.seen : n;  // keys that every row of the unit sees
 #pragma unroll
   for (int rg = 0; rg < RG; ++rg) {
-    const int row = it.row0 + rg * M + lm;
-    const int tok = divide(row, a.by_G);
-    valid[rg] = tok < it.q_len;
-    left[rg] = n;
-    if (a.causal && valid[rg] && tok + shift + 1 - it.c0 < n) left[rg] = tok + shift + 1 - it.c0;
-    const int head = kvh * G + (valid[rg] ? row - tok * G : 0);
-    const float* qp = static_cast<const float*>(a.q) + (it.q0 + (valid[rg] ? tok : 0)) * a.qt +
-                      (int64_t)head * a.qh + 4 * g;
+    const int r = rg * M + lm;
+    valid[rg] = r < it.rows;
+    const int x = it.head0 + (valid[rg] ? r : 0);
+    const int tok = divide(x, a.by_G);
+    left[rg] = valid[rg] && it.seen + tok < n ? it.seen + tok : n;
+    const float* qp = static_cast<const float*>(a.q) + (it.q_row + tok) * a.qt +
+                      (int64_t)(kvh * G + x - tok * G) * a.qh + 4 * g;
 #pragma unroll
     for (int i = 0; i < T::QI; ++i) {
-      const f32x4_t x = *reinterpret_cast<const f32x4_t*>(qp + 4 * T::G * i);
+      const f32x4_t q4 = *reinterpret_cast<const f32x4_t*>(qp + 4 * T::G * i);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) qr[rg * T::QI + i][e] = valid[rg] ? x[e] * a.scale_log2 : 0.f;
+      for (int e = 0; e < 4; ++e) qr[rg * T::QI + i][e] = valid[rg] ? q4[e] * a.scale_log2 : 0.f;
     }
   }
-  if (a.causal) {
-    const int first = divide(it.row0, a.by_G) + shift + 1 - it.c0;  // (the first row's)
-    whole = first < n ? first : n;
-  }
-
   const char* kb = reinterpret_cast<const char*>(static_cast<const float*>(a.k) +
-                                                 (it.k0 + it.c0) * a.kt + kvh * a.kh);
+                                                 it.k_row * a.kt + kvh * a.kh);
   const char* vb = reinterpret_cast<const char*>(static_cast<const float*>(a.v) +
-                                                 (it.k0 + it.c0) * a.vt + kvh * a.vh);
+                                                 it.k_row * a.vt + kvh * a.vh);
   const uint32_t ks = (uint32_t)a.kt * 4, vs = (uint32_t)a.vt * 4;
 
   float m[RG];
@@ -295,7 +282,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
     wgt[kWaves] = mm;
     return lt;
   };
-  const int64_t rows = (int64_t)it.q_len * G - it.row0;  // rows from the unit's first on
+  const int rows = it.rows;
   float wgt[kWaves + 1];
   if (tid < ROWS && tid < rows) {
     const float lf = (float)merged(tid, wgt);
@@ -303,8 +290,8 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
       const int64_t at = (int64_t)(it.part + tid) * a.H_kv + kvh;
       *reinterpret_cast<f32x2_t*>(a.part_ml + 2 * at) = f32x2_t{wgt[kWaves], lf};
     } else if (a.lse != nullptr) {
-      const int row = it.row0 + tid, tok = divide(row, a.by_G);
-      a.lse[(int64_t)(kvh * G + (row - tok * G)) * a.lse_head + it.q0 + tok] =
+      const int row = it.head0 + tid, tok = divide(row, a.by_G);
+      a.lse[(int64_t)(kvh * G + (row - tok * G)) * a.lse_head + it.q_row + tok] =
           lf == 0.f ? -INFINITY : (wgt[kWaves] + __log2f(lf)) * kLn2;
     }
   }
@@ -326,8 +313,8 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
     const float inv = lf == 0.f ? 0.f : 1.0f / lf;
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] *= inv;
-    const int row = it.row0 + r, tok = divide(row, a.by_G);
-    float* const op = static_cast<float*>(a.o) + (it.q0 + tok) * a.ot +
+    const int row = it.head0 + r, tok = divide(row, a.by_G);
+    float* const op = static_cast<float*>(a.o) + (it.q_row + tok) * a.ot +
                       (int64_t)(kvh * G + (row - tok * G)) * a.oh;
     *reinterpret_cast<f32x4_t*>(op + d4) = acc;
   }

@@ -48,44 +48,46 @@ Counts walk(const PackedSeqs& s, int block, Tile&& tile, Few&& few, Join&& join)
   Counts c = {0, 0, 0, 0};
   int64_t q0 = 0, k0 = 0;
   for (int i = 0; i < s.n; ++i) {
-    PackedItem it = {};
-    it.q0 = s.q_start ? s.q_start[i] : q0;
-    it.k0 = s.k_start ? s.k_start[i] : k0;
-    it.q_len = s.q_len[i];
-    it.k_len = s.k_len[i];
-    q0 += it.q_len;
-    k0 += it.k_len;
-    it.part = -1;
-    const int64_t rows = (int64_t)it.q_len * s.G;
+    const int64_t q_start = s.q_start ? s.q_start[i] : q0, k_start = s.k_start ? s.k_start[i] : k0;
+    const int q_len = s.q_len[i], k_len = s.k_len[i];
+    q0 += q_len;
+    k0 += k_len;
+    const int shift = k_len - q_len;  // causal: token t sees keys up to t + shift
+    const int64_t rows = (int64_t)q_len * s.G;
     if (rows == 0) continue;
+    PackedItem it = {};
+    it.part = -1;
     if (rows > kPackedFew[s.bf16]) {
       for (int64_t r = 0; r < rows; r += block) {
-        it.row0 = (int)r;
-        it.c0 = 0;
-        it.c1 = it.k_len;
-        if (s.causal) {
-          // the last row's last key
-          const int64_t tok = std::min<int64_t>(it.q_len - 1, (r + block - 1) / s.G);
-          it.c1 = (int)std::max<int64_t>(0, std::min<int64_t>(it.k_len, tok + it.k_len - it.q_len + 1));
-        }
+        const int tok = (int)(r / s.G);
+        const int last = (int)std::min<int64_t>(q_len - 1, (r + block - 1) / s.G);
+        it.q_row = q_start + tok;
+        it.head0 = (int)(r - (int64_t)tok * s.G);
+        it.rows = (int)(rows - r);
+        it.keys = s.causal ? std::max(0, std::min(k_len, last + shift + 1)) : k_len;
+        it.seen = s.causal ? tok + shift + 1 : kAllSeen;
+        it.k_row = it.keys > 0 ? k_start : 0;
         tile(it);
         ++c.tiles;
       }
       continue;
     }
-    const int keys = part_keys(s.bf16, it.k_len);
-    const int parts = std::max(1, (int)(((int64_t)it.k_len + keys - 1) / keys));
+    const int keys = part_keys(s.bf16, k_len);
+    const int parts = std::max(1, (int)(((int64_t)k_len + keys - 1) / keys));
+    it.q_row = q_start;
+    it.rows = (int)rows;
     for (int p = 0; p < parts; ++p) {
-      it.row0 = 0;
-      it.c0 = p * keys;
-      it.c1 = std::min(it.k_len, it.c0 + keys);
+      const int first = p * keys;
+      it.keys = std::min(k_len - first, keys);
+      it.k_row = it.keys > 0 ? k_start + first : 0;
+      it.seen = s.causal ? shift + 1 - first : kAllSeen;
       if (parts > 1) it.part = (int)(c.part_rows + p * rows);
       few(it);
       ++c.few;
     }
     if (parts > 1) {
       for (int64_t r = 0; r < rows; ++r) {
-        join(PackedJoin{it.q0 + r / s.G, (int)(r % s.G), (int)(c.part_rows + r), (int)rows, parts});
+        join(PackedJoin{q_start + r / s.G, (int)(r % s.G), (int)(c.part_rows + r), (int)rows, parts});
         ++c.joins;
       }
       c.part_rows += parts * rows;
@@ -121,10 +123,9 @@ void packed_fill(const PackedSeqs& s, const PackedCounts& n, void* plan) {
   // longest first, so that the launch's tail is made of short units; order changes only
   // the schedule.  (std::sort: no allocation)
   auto longer = [](const PackedItem& a, const PackedItem& b) {
-    const int la = a.c1 - a.c0, lb = b.c1 - b.c0;
-    if (la != lb) return la > lb;
-    if (a.q0 != b.q0) return a.q0 < b.q0;
-    return a.row0 != b.row0 ? a.row0 < b.row0 : a.c0 < b.c0;
+    if (a.keys != b.keys) return a.keys > b.keys;
+    if (a.q_row != b.q_row) return a.q_row < b.q_row;
+    return a.head0 != b.head0 ? a.head0 < b.head0 : a.k_row < b.k_row;
   };
   std::sort(tiles, tiles + n.tiles, longer);
   std::sort(few, few + n.few, longer);

@@ -16,8 +16,8 @@ def L():
     return losa
 
 
-ITEM = np.dtype([("q0", "<i8"), ("k0", "<i8"), ("q_len", "<i4"), ("k_len", "<i4"), ("row0", "<i4"),
-                 ("c0", "<i4"), ("c1", "<i4"), ("part", "<i4")])
+ITEM = np.dtype([("q_row", "<i8"), ("k_row", "<i8"), ("head0", "<i4"), ("rows", "<i4"), ("keys", "<i4"),
+                 ("seen", "<i4"), ("part", "<i4"), ("unused", "<i4")])
 JOIN = np.dtype([("q_row", "<i8"), ("in_group", "<i4"), ("part", "<i4"), ("step", "<i4"), ("n", "<i4")])
 
 
@@ -44,39 +44,52 @@ def test_units_cover_every_row_and_key_once(L, dtype, causal, seed):
     parts = []
     q0 = k0 = 0
     for q, k in zip(ql, kl):
-        rows = q * G
-        mine = [x for x in tiles if x["q0"] == q0 and x["q_len"] == q and q] if rows > most else []
-        split = [x for x in few if x["q0"] == q0 and x["q_len"] == q] if 0 < rows <= most else []
-        for x in list(mine) + list(split):
-            assert x["k0"] == k0 and x["k_len"] == k
-        if rows > most:
-            assert sorted(x["row0"] for x in mine) == list(range(0, rows, block))
-            for x in mine:
-                last = min(q - 1, (int(x["row0"]) + block - 1) // G)
-                assert x["c0"] == 0 and x["part"] == -1
-                assert x["c1"] == (max(0, min(k, last + k - q + 1)) if causal else k)
-        elif rows:
-            split = sorted(split, key=lambda x: x["c0"])
-            edges = [(int(x["c0"]), int(x["c1"])) for x in split]
-            assert edges[0][0] == 0 and edges[-1][1] == k
-            assert all(a[1] == b[0] for a, b in zip(edges, edges[1:])) and len(edges) <= 256
-            if len(split) == 1:
-                assert split[0]["part"] == -1
+        rows, shift = q * G, k - q
+        sees = lambda t: max(0, min(k, t + shift + 1)) if causal else k  # noqa: E731
+        mine = [x for x in (tiles if rows > most else few) if q0 <= x["q_row"] < q0 + q]
+        number = lambda x: (int(x["q_row"]) - q0) * G + int(x["head0"])  # noqa: E731
+        for x in mine:
+            assert int(x["rows"]) == rows - number(x)
+            if x["keys"]:
+                assert k0 <= x["k_row"] and x["k_row"] + x["keys"] <= k0 + k
             else:
-                first = int(split[0]["part"])
-                assert [int(x["part"]) for x in split] == [first + i * rows for i in range(len(split))]
+                assert x["k_row"] == 0
+            # each row's keys, as the kernels read them, are those of the formula that the
+            # unit's range holds
+            c0 = int(x["k_row"]) - k0 if x["keys"] else 0
+            for r in (0, min(block, int(x["rows"])) - 1):
+                t = (int(x["head0"]) + r) // G
+                tok = int(x["q_row"]) - q0 + t
+                assert max(0, min(int(x["keys"]), int(x["seen"]) + t)) == \
+                    max(0, min(c0 + int(x["keys"]), sees(tok)) - c0)
+        if rows > most:
+            assert sorted(map(number, mine)) == list(range(0, rows, block))
+            for x in mine:
+                last = min(q - 1, (number(x) + block - 1) // G)
+                assert x["part"] == -1 and x["keys"] == sees(last)
+                assert x["keys"] == 0 or x["k_row"] == k0
+        elif rows:
+            mine = sorted(mine, key=lambda x: x["k_row"])
+            assert all(number(x) == 0 for x in mine) and sum(int(x["keys"]) for x in mine) == k
+            assert len(mine) <= 256 and (k == 0 or mine[0]["k_row"] == k0)
+            assert all(a["k_row"] + a["keys"] == b["k_row"] for a, b in zip(mine, mine[1:]))
+            if len(mine) == 1:
+                assert mine[0]["part"] == -1
+            else:
+                first = int(mine[0]["part"])
+                assert [int(x["part"]) for x in mine] == [first + i * rows for i in range(len(mine))]
                 got = [j for j in joins if q0 <= j["q_row"] < q0 + q]
                 assert sorted((int(j["q_row"]) - q0) * G + int(j["in_group"]) for j in got) == list(range(rows))
                 for j in got:
                     r = (int(j["q_row"]) - q0) * G + int(j["in_group"])
-                    assert (j["part"], j["step"], j["n"]) == (first + r, rows, len(split))
-                parts.append((first, first + len(split) * rows))
+                    assert (j["part"], j["step"], j["n"]) == (first + r, rows, len(mine))
+                parts.append((first, first + len(mine) * rows))
         q0, k0 = q0 + q, k0 + k
     parts.sort()
     assert sum(b - a for a, b in parts) == p.info.part_rows
     assert all(a[1] == b[0] for a, b in zip(parts, parts[1:]))
     for x in (tiles, few):  # longest first
-        n = [int(y["c1"]) - int(y["c0"]) for y in x]
+        n = [int(y["keys"]) for y in x]
         assert n == sorted(n, reverse=True)
     assert p.workspace_bytes(128) == p.info.part_rows * 2 * 130 * 4
 
@@ -84,8 +97,9 @@ def test_units_cover_every_row_and_key_once(L, dtype, causal, seed):
 def test_a_sequence_is_split_alike_in_any_batch(L):
     alone = units(L.losa_packed_plan([3], [9000], 8, 2, torch.bfloat16, device="cpu"))[1]
     among = units(L.losa_packed_plan([500, 3, 1], [20, 9000, 40_000], 8, 2, torch.bfloat16, device="cpu"))[1]
-    cut = lambda x: sorted((int(y["c0"]), int(y["c1"])) for y in x if y["k_len"] == 9000)  # noqa: E731
-    assert cut(alone) == cut(among)
+    cut = lambda x, k0: sorted((int(y["k_row"]) - k0, int(y["keys"])) for y in x  # noqa: E731
+                               if k0 <= y["k_row"] < k0 + 9000)
+    assert cut(alone, 0) == cut(among, 20) and len(alone) > 1
 
 
 def test_nothing_to_do(L):
