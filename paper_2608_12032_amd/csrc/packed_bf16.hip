@@ -685,9 +685,8 @@ constexpr int packed_waves_per_simd() {
   return D == 64 ? 4 : 2;
 }
 
-// Tiles come first in a plan, then few-row parts.  At d = 128 one kernel runs both (10
-// prompts of 1 to 1,024 tokens: 33.8 us, in two launches 39.8).  At d = 64 the tiles' 128
-// registers leave no room for that (142 us alone, 200 in one kernel: it spills).
+// Tiles come first in a plan, then few-row parts: each kind in a kernel of its own, or
+// both in one (kTogether).
 constexpr int kTiles = 1, kFew = 2;
 template <int D, int KINDS>
 __global__ void __launch_bounds__(64 * NW)
@@ -784,24 +783,30 @@ void launch_units(const PackedArgs& a, int units, hipStream_t stream) {
                        dim3(64 * NW), 0, stream, a);
 }
 
-hipError_t launch_64(const PackedArgs& a, int n_few, hipStream_t stream) {
-  launch_units<64, kTiles>(a, a.n_tiles, stream);
-  PackedArgs few = a;
-  few.items += a.n_tiles;
-  launch_units<64, kFew>(few, n_few, stream);
-  return hipGetLastError();
-}
+// Tiles of a call up to which both kinds share a launch at d = 128: it saves 3.4 us (10
+// prompts of 1 to 1,024 tokens x 32 / 8 heads, 246 x 8 tiles: 31.3 us, in two launches
+// 34.7), and the tiles are 2 % slower in it (12 heads x 8,192 dense: 370 / 361 us).  At
+// d = 64, where a kernel of both spills, they are 10 to 15 % slower.
+constexpr int64_t kTogether = 4096;
 
-hipError_t launch_128(const PackedArgs& a, int n_few, hipStream_t stream) {
-  launch_units<128, kTiles | kFew>(a, a.n_tiles + n_few, stream);
+template <int D>
+hipError_t launch(const PackedArgs& a, int n_few, hipStream_t stream) {
+  if (D == 128 && a.n_tiles > 0 && n_few > 0 && (int64_t)a.n_tiles * a.H_kv <= kTogether) {
+    launch_units<128, kTiles | kFew>(a, a.n_tiles + n_few, stream);
+  } else {
+    launch_units<D, kTiles>(a, a.n_tiles, stream);
+    PackedArgs few = a;
+    few.items += a.n_tiles;
+    launch_units<D, kFew>(few, n_few, stream);
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_packed_bf16(int d, const PackedArgs& a, int n_few, hipStream_t stream) {
-  if (d == 64) return launch_64(a, n_few, stream);
-  if (d == 128) return launch_128(a, n_few, stream);
+  if (d == 64) return launch<64>(a, n_few, stream);
+  if (d == 128) return launch<128>(a, n_few, stream);
   return hipErrorInvalidValue;
 }
 
