@@ -176,6 +176,7 @@ losa_status losa_packed_attn_fwd(const losa_view* q, const losa_view* k, const l
   a.lse_head = lse_head;
   a.q_rows = q_rows;
   a.k_rows = k_rows;
+  a.part_rows = info->part_rows;
   a.H_kv = info->H_kv;
   a.G = info->H / info->H_kv;
   a.by_G = losa::fast_div((uint32_t)a.G);

@@ -105,6 +105,12 @@ losa_status check_rotation(const losa_rotation* r, int N, int d, losa::RowsArgs*
   return LOSA_OK;
 }
 
+losa_status rows_status(hipError_t e, const char* what) {
+  if (e == hipErrorInvalidConfiguration)
+    return fail(LOSA_ERR_INVALID_SHAPE, "%s: more workgroups than one launch takes", what);
+  return hip_status(e, what);
+}
+
 void set_tensor(losa::RowsTensor* t, const losa_view& x, const losa_view& y, int H) {
   t->x = x.data;
   t->xb = x.batch;
@@ -160,7 +166,7 @@ losa_status losa_rope(const losa_view* x, losa_dtype dtype, int B, int N, int N_
   a.n_pad = N_pad;
   set_tensor(&a.t[0], xv, yv, H);
   a.t[0].rotate = 1;
-  return hip_status(losa::launch_rows(d, dtype == LOSA_DTYPE_BF16,
+  return rows_status(losa::launch_rows(d, dtype == LOSA_DTYPE_BF16,
                                       rot->pairs == LOSA_PAIRS_HALVES, a, 1, false,
                                       static_cast<hipStream_t>(stream)),
                     "losa_rope");
@@ -214,7 +220,7 @@ losa_status losa_qk_norm_rope(const losa_view* q, const losa_view* k, const losa
     a.t[1].w = norm->k_weight;
     a.t[1].b = norm->k_bias;
   }
-  return hip_status(losa::launch_rows(d, dtype == LOSA_DTYPE_BF16,
+  return rows_status(losa::launch_rows(d, dtype == LOSA_DTYPE_BF16,
                                       rot && rot->pairs == LOSA_PAIRS_HALVES, a, v ? 3 : 2, all,
                                       static_cast<hipStream_t>(stream)),
                     "losa_qk_norm_rope");

@@ -54,19 +54,28 @@ struct PackedArgs {
   float *part_o, *part_ml;               // [partial row][H_kv][d], [...][2]: max (log2 units), sum
   int64_t qt, qh, kt, kh, vt, vh, ot, oh;  // token and head strides, elements
   int64_t lse_head;
-  int64_t q_rows, k_rows;
+  int64_t q_rows, k_rows, part_rows;
   int H_kv, G;
   FastDiv by_G, by_H_kv;
   int n_tiles;  // items below this are tiles, the others parts of few-row sequences
   int tile_rows;
   float scale_log2;
 };
-// Whether the unit's rows (`tile` at most) and keys lie inside q and k.  (A plan's do;
-// nothing is read or written for one that does not.)
+// Whether the unit's rows (`tile` at most), keys and partial rows lie inside q, k and the
+// workspace, and a join's inside q and the workspace.  (A plan's do; nothing is read or
+// written for one that does not.)
 __device__ __forceinline__ bool inside(const PackedArgs& a, const PackedItem& it, int tile) {
   const int last = it.head0 + (it.rows < tile ? it.rows : tile) - 1;
-  return (it.q_row >= 0) & (it.k_row >= 0) & (it.head0 >= 0) & (it.rows > 0) & (it.keys >= 0) &
-         (it.q_row + divide(last, a.by_G) < a.q_rows) & (it.k_row + it.keys <= a.k_rows);
+  return (it.q_row >= 0) & (it.k_row >= 0) & (it.head0 >= 0) & (it.head0 < a.G) & (it.rows > 0) &
+         (it.keys >= 0) &
+         (it.q_row + divide(last, a.by_G) < a.q_rows) & (it.k_row + it.keys <= a.k_rows) &
+         ((it.part < 0) | ((it.rows <= tile) & ((int64_t)it.part + it.rows <= a.part_rows)));
+}
+constexpr int kMostParts = 256;
+__device__ __forceinline__ bool inside(const PackedArgs& a, const PackedJoin& j) {
+  return (j.q_row >= 0) & (j.q_row < a.q_rows) & (j.in_group >= 0) & (j.in_group < a.G) &
+         (j.part >= 0) & (j.step >= 0) & (j.n > 0) & (j.n <= kMostParts) &
+         (j.part + (int64_t)(j.n - 1) * j.step < a.part_rows);
 }
 
 // Rows of a tile (fp32: of a wide one; a call of few units takes tiles of 16), rows of

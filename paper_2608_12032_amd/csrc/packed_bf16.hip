@@ -704,7 +704,7 @@ __global__ void __launch_bounds__(64 * NW)
 // max and adds them in order; the waves' states are then merged in order.  The outputs'
 // loads do not wait for the weights.
 constexpr int kJoinWaves = 8;
-constexpr int kJoinMost = 32;  // parts of a wave: a plan has 256 at most
+constexpr int kJoinMost = kMostParts / kJoinWaves;  // parts of a wave
 
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(const PackedArgs a) {
@@ -714,11 +714,12 @@ __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(const PackedArgs 
   const int unit = divide((int)blockIdx.x, a.by_H_kv);
   const int kvh = (int)blockIdx.x - unit * a.H_kv;
   const PackedJoin j = a.joins[unit];
+  if (!inside(a, j)) return;
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   auto at = [&](int i) { return (int64_t)(j.part + (int64_t)i * j.step) * a.H_kv + kvh; };
   int n = (j.n - w + kJoinWaves - 1) / kJoinWaves;  // parts of this wave
-  n = n < 0 ? 0 : (n > kJoinMost ? kJoinMost : n);
+  static_assert(kJoinMost <= 64, "a lane for each part of a wave");
   f32x2_t mine = {kNegBig, 0.f};
   if (lane < n) mine = *reinterpret_cast<const f32x2_t*>(a.part_ml + 2 * at(w + kJoinWaves * lane));
   float acc[PL] = {};

@@ -16,7 +16,7 @@ namespace {
 // join stays short.
 int part_keys(bool bf16, int k_len) {
   const int least = bf16 ? 256 : 512;
-  const int64_t even = ((int64_t)k_len + 255) / 256;
+  const int64_t even = ((int64_t)k_len + kMostParts - 1) / kMostParts;
   const int64_t keys = (even + 63) / 64 * 64;
   return (int)(keys < least ? least : keys);
 }

@@ -252,6 +252,38 @@ def test_what_a_row_does_not_see_does_not_reach_it(L, dtype, bad):
                 assert not torch.isfinite(seen).any()
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_no_key_at_all(L, dtype):
+    """k and v without a row; rows that see nothing are 0, their lse -inf."""
+    q = randn(40, 4, 64, seed=60, dtype=dtype).cuda()
+    k = torch.empty(0, 2, 64, dtype=dtype, device="cuda")
+    for causal in (False, True):
+        for ql in ([40], [1, 39], [16, 24]):
+            o, lse = call(L, q, k, k, ql, [0] * len(ql), causal, k_starts=[99] * len(ql),
+                          out=torch.full_like(q, 2.0))
+            assert not o.any() and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_a_plan_that_is_none_writes_nothing(L, dtype):
+    """Units and joins outside q, k and the workspace are passed over."""
+    d, ql, kl = 128, [3, 200], [3000, 200]
+    q = randn(sum(ql), 4, d, seed=61, dtype=dtype).cuda()
+    k, v = (randn(sum(kl), 2, d, seed=s, dtype=dtype).cuda() for s in (62, 63))
+    plan = L.losa_packed_plan(ql, kl, 4, 2, dtype, causal=True)
+    good = plan.data.clone()
+    ws = plan.workspace(d)
+    for fill in (-1, 0x7f7f7f7f7f7f7f7f, 1 << 40):
+        plan.data.fill_(fill)
+        ws.zero_()
+        out, lse = torch.full_like(q, 5.0), torch.full((4, sum(ql)), 6.0, device="cuda")
+        L.losa_packed_attn_fwd(q, k, v, plan, want_lse=True, out=out, lse=lse, workspace=ws)
+        assert (out == 5).all() and (lse == 6).all() and not ws.any(), fill
+    plan.data.copy_(good)
+    want, _ = call(L, q, k, v, ql, kl, True)
+    assert torch.equal(L.losa_packed_attn_fwd(q, k, v, plan), want)
+
+
 def test_infinite_value_of_one_channel(L):
     """One infinite value at one key: only that channel, only the rows that see it."""
     for dtype in (BF, F):

@@ -98,6 +98,9 @@ ROPE_CASES = [  # dtype, d, halves, dims, grid, text, B, H, pad
     ("f32", 128, True, (128,), (1, 1, 130), 0, 1, 4, 64),
     ("f32", 64, False, (8, 8, 8, 8), (2, 3, 5), 0, 1, 3, 1),    # four axes
     ("f32", 64, True, (16, 24, 24), (3, 3, 3), 1, 2, 40, 128),
+    ("bf16", 64, True, (6, 10), (1, 5, 9), 2, 1, 3, 1),         # pairs of a lane on two axes
+    ("bf16", 128, False, (2, 2, 4), (2, 3, 4), 1, 1, 2, 1),
+    ("f32", 128, True, (10, 2, 44), (3, 2, 7), 0, 2, 6, 128),
     ("bf16", 128, False, (128,), (1, 1, 1), 0, 1, 1, 1),        # one token, one head
     ("f32", 64, False, (64,), (1, 1, 1), 0, 5, 2, 1),
 ]
