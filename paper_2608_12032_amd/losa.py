@@ -416,14 +416,20 @@ def losa_construct(q, k, v, N: int, block_q: int, block_k: int | None = None,
 
 class RopeTable:
     """Cosines and sines by axis and position, on a device: what losa_rope_table returns.
-    ``data`` fp32; ``axis_dim`` and ``axis_len`` as given."""
+    ``data`` fp32 (not to be replaced); ``axis_dim`` and ``axis_len`` as given."""
 
     def __init__(self, data, axis_dim, axis_len):
-        self.data, self.axis_dim, self.axis_len = data, tuple(axis_dim), tuple(axis_len)
+        self._data, self.axis_dim, self.axis_len = data, tuple(axis_dim), tuple(axis_len)
+        floats = sum(a * b for a, b in zip(self.axis_dim, self.axis_len))
+        if data.dtype != torch.float32 or not data.is_contiguous() or data.numel() < floats:
+            raise ValueError(f"data must be contiguous fp32 of {floats} elements")
         self._axes = len(self.axis_dim)
         rest = (0,) * (MAX_AXES - self._axes)
         self._head = _AXES(self._axes, *self.axis_dim, *rest, *self.axis_len, *rest)
-        self._floats = sum(a * b for a, b in zip(self.axis_dim, self.axis_len))
+
+    @property
+    def data(self):
+        return self._data
 
 
 def losa_rope_table(axis_dim, axis_len, base: float = 10000.0, device="cuda") -> RopeTable:
@@ -480,8 +486,9 @@ def _rotation(table, pos, pairing, B, N, device):
     """losa_rotation of a table and positions int32 [axes, N] or [B, axes, N]."""
     if not isinstance(table, RopeTable):
         raise TypeError("table must be a RopeTable (losa_rope_table)")
-    n, data = table._axes, table.data
-    _arg(data, "table", device, dtype=torch.float32, numel=table._floats)
+    n, data = table._axes, table._data
+    if data.device != device:
+        raise ValueError(f"table must live on {device} (got {data.device})")
     _arg(pos, "pos", device, dtype=torch.int32)
     shape = pos.shape
     if shape == (n, N):
@@ -585,14 +592,19 @@ def losa_qk_norm_rope(q, k, v=None, *, norm: str | None = "rms", over: str = "he
 
 class PackedPlan:
     """Plan of a batch of packed sequences on a device: what losa_packed_plan returns.
-    ``info`` holds its sizes (losa_packed_info), ``data`` the units of work."""
+    ``info`` holds its sizes (losa_packed_info), ``data`` the units of work (neither to be
+    replaced)."""
 
     def __init__(self, info, data, dtype):
-        self.info, self.data, self.dtype = info, data, dtype
+        self.info, self._data, self.dtype = info, data, dtype
         self.q_rows, self.k_rows = info.q_rows, info.k_rows
         self.heads, self.kv_heads = info.H, info.H_kv
         self._at = ctypes.addressof(info)
         self._need = {d: int(lib.losa_packed_workspace_bytes(self._at, d)) for d in (64, 128)}
+
+    @property
+    def data(self):
+        return self._data
 
     def workspace_bytes(self, d: int) -> int:
         return self._need.get(d, 0)
@@ -600,7 +612,7 @@ class PackedPlan:
     def workspace(self, d: int):
         """A workspace for losa_packed_attn_fwd at head dim d, None where it needs none."""
         need = self.workspace_bytes(d)
-        return torch.empty(need, dtype=torch.uint8, device=self.data.device) if need else None
+        return torch.empty(need, dtype=torch.uint8, device=self._data.device) if need else None
 
 
 def losa_packed_plan(q_lens, k_lens, heads: int, kv_heads: int, dtype, causal: bool = False,
@@ -663,8 +675,8 @@ def losa_packed_attn_fwd(q, k, v, plan: PackedPlan, scale: float | None = None,
     shape, shape_kv = (rows, plan.heads, d), (k_rows, plan.kv_heads, d)
     if not q.is_cuda:
         raise ValueError(f"q must live on a GPU (got {dev})")
-    if plan.data.device != dev:
-        raise ValueError(f"the plan must live on {dev} (got {plan.data.device})")
+    if plan._data.device != dev:
+        raise ValueError(f"the plan must live on {dev} (got {plan._data.device})")
     qv = _packed_view(q, "q", dev, dt, shape)
     kv = _packed_view(k, "k", dev, dt, shape_kv)
     vv = _packed_view(v, "v", dev, dt, shape_kv)
@@ -684,7 +696,7 @@ def losa_packed_attn_fwd(q, k, v, plan: PackedPlan, scale: float | None = None,
         _arg(workspace, "workspace", dev, nbytes=need)
         ws_at, ws_bytes = workspace.data_ptr(), workspace.nbytes
     st = _call(dev, lib.losa_packed_attn_fwd, qv, kv, vv, rows, k_rows, plan._at,
-               plan.data.data_ptr(), d, 1.0 / math.sqrt(d) if scale is None else scale, ov, lse_at,
+               plan._data.data_ptr(), d, 1.0 / math.sqrt(d) if scale is None else scale, ov, lse_at,
                rows, ws_at, ws_bytes)
     if st:
         _check(st, "losa_packed_attn_fwd")

@@ -44,6 +44,14 @@ def test_table_refusals(L, dims, lens, base, status):
     assert e.value.status == status
 
 
+def test_a_table_holds_its_positions(L):
+    for data in (torch.zeros(75), torch.zeros(76, dtype=torch.float64), torch.zeros(152)[::2]):
+        with pytest.raises(ValueError, match="76 elements"):
+            L.RopeTable(data, (4, 6), (7, 8))
+    with pytest.raises(AttributeError):
+        L.RopeTable(torch.zeros(76), (4, 6), (7, 8)).data = torch.zeros(1)
+
+
 def test_table_capacity(L):
     room = (ctypes.c_float * 8)()
     one = lambda *x: (ctypes.c_int * len(x))(*x)  # noqa: E731
@@ -74,7 +82,7 @@ def test_structures_are_packed_as_c_lays_them_out(L):
     """The binding passes structures as bytes: the layout a C compiler gives them."""
     ints = ctypes.c_int * 4
     assert bytes(View(1 << 40, 2, 3, 4)) == L._VIEW(1 << 40, 2, 3, 4)
-    t = L.RopeTable(None, (4, 6), (7, 8))
+    t = L.RopeTable(torch.zeros(76), (4, 6), (7, 8))
     assert bytes(Rotation(2, ints(4, 6), ints(7, 8), 1 << 33, 1 << 34, 9, 1)) == \
         t._head + L._ROTATION(1 << 33, 1 << 34, 9, 1)
     assert bytes(QkNorm(2, 1, 0.5, 1 << 33, None, 8, 1 << 50)) == \
