@@ -391,7 +391,8 @@ typedef struct {
   int64_t bytes;          /* of the plan                                                   */
   int64_t q_rows, k_rows; /* rows that q and o, and k and v, must have                     */
   int64_t part_rows;      /* rows of partial results (the workspace's size)                */
-  int32_t n_tiles, n_few, n_joins; /* units of work                                        */
+  int32_t n_tiles, n_few;          /* units of work: tiles of tile_rows rows, parts of few  */
+  int32_t n_joins, n_wide;         /* rows joined from parts, those of many parts          */
   int32_t tile_rows;
   int32_t H, H_kv, causal;
   losa_dtype dtype;
@@ -410,9 +411,10 @@ typedef struct {
  * plan              NULL: only `info` is filled.  Else at least info->bytes bytes,
  *                   8-byte aligned.
  * H must be a multiple of H_kv.
- * A sequence's rows are q_len * H / H_kv per key head.  Few rows (bf16 32 or fewer, f32
- * 16) split its keys into parts that are joined; how follows from its own lengths and
- * H / H_kv alone, so a sequence gives the same bits alone and packed among others.
+ * A sequence's rows are q_len * H / H_kv per key head.  Few rows (up to 2,048 in bf16, 512
+ * in f32) over many keys split the keys into parts that are joined; how follows from its
+ * own lengths and H / H_kv alone, so a sequence gives the same bits alone and packed
+ * among others.
  */
 losa_status losa_packed_plan(const int64_t* q_start, const int32_t* q_len, const int64_t* k_start,
                              const int32_t* k_len, int n_seq, losa_dtype dtype, int H, int H_kv,

@@ -40,9 +40,9 @@ losa_status check_disjoint(const int64_t* start, const int32_t* len, int n) {
 
 bool info_ok(const losa_packed_info* i) {
   return i->bytes >= 0 && i->q_rows >= 0 && i->k_rows >= 0 && i->part_rows >= 0 && i->n_tiles >= 0 &&
-         i->n_few >= 0 && i->n_joins >= 0 && i->H > 0 && i->H_kv > 0 && i->H % i->H_kv == 0 &&
+         i->n_few >= 0 && i->n_wide >= 0 && i->n_joins >= i->n_wide && i->H > 0 && i->H_kv > 0 && i->H % i->H_kv == 0 &&
          (i->dtype == LOSA_DTYPE_F32 || i->dtype == LOSA_DTYPE_BF16) &&
-         (size_t)i->bytes == losa::packed_plan_bytes({i->n_tiles, i->n_few, i->n_joins, i->tile_rows, i->part_rows}) &&
+         (size_t)i->bytes == losa::packed_plan_bytes({i->n_tiles, i->n_few, i->n_joins, i->n_wide, i->tile_rows, i->part_rows}) &&
          (i->tile_rows == losa::kPackedTile[i->dtype == LOSA_DTYPE_BF16] ||
           (i->dtype == LOSA_DTYPE_F32 && i->tile_rows == losa::kPackedNarrow));
 }
@@ -83,7 +83,7 @@ losa_status losa_packed_plan(const int64_t* q_start, const int32_t* q_len, const
   if (!losa::packed_counts(s, &c))
     return fail(LOSA_ERR_INVALID_SHAPE, "the batch has more units of work than one launch takes");
   const losa_packed_info got = {(int64_t)losa::packed_plan_bytes(c), q_rows, k_rows, c.part_rows,
-                                c.tiles, c.few, c.joins, c.tile_rows, H, H_kv, causal != 0,
+                                c.tiles, c.few, c.joins, c.wide, c.tile_rows, H, H_kv, causal != 0,
                                 dtype};
   if (plan) {
     if ((reinterpret_cast<uintptr_t>(plan) & 7u) != 0)
@@ -182,13 +182,15 @@ losa_status losa_packed_attn_fwd(const losa_view* q, const losa_view* k, const l
   a.by_G = losa::fast_div((uint32_t)a.G);
   a.by_H_kv = losa::fast_div((uint32_t)a.H_kv);
   a.n_tiles = info->n_tiles;
+  a.n_joins = info->n_joins;
+  a.n_wide = info->n_wide;
   a.tile_rows = info->tile_rows;
   a.scale_log2 = scale * 1.4426950408889634f;
   hipStream_t hs = static_cast<hipStream_t>(stream);
   st = hip_status((bf16 ? losa::launch_packed_bf16 : losa::launch_packed_f32)(d, a, info->n_few, hs),
                   "losa_packed_attn_fwd");
   if (st != LOSA_OK) return st;
-  return hip_status(losa::launch_packed_join(d, bf16, a, info->n_joins, hs),
+  return hip_status(losa::launch_packed_join(d, bf16, a, hs),
                     "losa_packed_attn_fwd (join)");
 }
 

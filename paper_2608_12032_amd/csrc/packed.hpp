@@ -58,6 +58,7 @@ struct PackedArgs {
   int H_kv, G;
   FastDiv by_G, by_H_kv;
   int n_tiles;  // items below this are tiles, the others parts of few-row sequences
+  int n_joins, n_wide;  // rows to join; the first n_wide are of more than kFewParts parts
   int tile_rows;
   float scale_log2;
 };
@@ -65,13 +66,13 @@ struct PackedArgs {
 // workspace, and a join's inside q and the workspace.  (A plan's do; nothing is read or
 // written for one that does not.)
 __device__ __forceinline__ bool inside(const PackedArgs& a, const PackedItem& it, int tile) {
-  const int last = it.head0 + (it.rows < tile ? it.rows : tile) - 1;
+  const int rows = it.rows < tile ? it.rows : tile;
   return (it.q_row >= 0) & (it.k_row >= 0) & (it.head0 >= 0) & (it.head0 < a.G) & (it.rows > 0) &
          (it.keys >= 0) &
-         (it.q_row + divide(last, a.by_G) < a.q_rows) & (it.k_row + it.keys <= a.k_rows) &
-         ((it.part < 0) | ((it.rows <= tile) & ((int64_t)it.part + it.rows <= a.part_rows)));
+         (it.q_row + divide(it.head0 + rows - 1, a.by_G) < a.q_rows) & (it.k_row + it.keys <= a.k_rows) &
+         ((it.part < 0) | ((int64_t)it.part + rows <= a.part_rows));
 }
-constexpr int kMostParts = 256;
+constexpr int kMostParts = 256, kFewParts = 16;
 __device__ __forceinline__ bool inside(const PackedArgs& a, const PackedJoin& j) {
   return (j.q_row >= 0) & (j.q_row < a.q_rows) & (j.in_group >= 0) & (j.in_group < a.G) &
          (j.part >= 0) & (j.step >= 0) & (j.n > 0) & (j.n <= kMostParts) &
@@ -91,7 +92,7 @@ struct PackedSeqs {
   bool bf16;
 };
 struct PackedCounts {
-  int tiles, few, joins;
+  int tiles, few, joins, wide;
   int tile_rows;
   int64_t part_rows;
 };
@@ -103,6 +104,6 @@ inline size_t packed_plan_bytes(const PackedCounts& n) {
 }
 hipError_t launch_packed_bf16(int d, const PackedArgs& a, int n_few, hipStream_t stream);
 hipError_t launch_packed_f32(int d, const PackedArgs& a, int n_few, hipStream_t stream);
-hipError_t launch_packed_join(int d, bool bf16, const PackedArgs& a, int n_joins, hipStream_t stream);
+hipError_t launch_packed_join(int d, bool bf16, const PackedArgs& a, hipStream_t stream);
 
 }  // namespace losa

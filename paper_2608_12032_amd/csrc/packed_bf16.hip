@@ -5,8 +5,8 @@
 //   O = sum_j softmax_j(scale q . k_j) v_j over the keys j it sees (causal:
 //   j <= i + k_len - q_len), by the online softmax: running max, sum and O^T.
 //
-// Work unit.  One workgroup owns 32 NW rows of one sequence and key head and walks a
-// range of its keys.  Rows are numbered token * G + head in group, so a tile's rows
+// Work unit.  A workgroup of four waves owns a tile of 128 rows, 32 a wave, of one sequence
+// and key head and walks a range of its keys.  Rows are numbered token * G + head in group, so a tile's rows
 // share their keys whatever G is: G heads of one token fill a tile where each alone
 // would leave it nearly empty.  The plan lists the units, longest first.  Orientation,
 // key order, LDS images, the two rings and the pipelined sub-iteration are those of
@@ -15,9 +15,11 @@
 //
 // Sequences of few rows (32 or fewer: single tokens with grouped heads) are bound by
 // HBM, K and V read once, and have no rows to fill the chip with: their keys are split
-// into parts (packed_plan.cpp), one wave each (NW = 1, its own rings), whose O, max and
-// sum are joined in a fixed order by join_kernel.  How a sequence is split follows from
-// its own lengths alone, so it gives the same bits alone and packed among others.
+// into parts (packed_plan.cpp) of a workgroup each, whose waves take the sub-tiles in turn.
+// Where few tiles meet many keys, their keys are split too.  Parts leave O, max and sum in
+// the workspace, and join_kernel joins them in a fixed order.  How a sequence is split
+// follows from its own lengths alone, so it gives the same bits alone and packed among
+// others.
 //
 // Bounds.  K and V are read through a buffer resource of one sub-tile each, cut at the
 // unit's last key and rebuilt per sub-tile from 64-bit addresses: rows behind the end
@@ -278,6 +280,13 @@ __device__ __forceinline__ RowOut row_out(const PackedArgs& a, const PackedItem&
   return r;
 }
 
+// The same of a row's partial result: elements of part_o and part_ml.
+template <int D>
+__device__ __forceinline__ RowOut part_out(const PackedArgs& a, const PackedItem& it, int r, int kvh) {
+  const int64_t at = (int64_t)(it.part + r) * a.H_kv + kvh;
+  return {at * D, 2 * at};
+}
+
 constexpr int NW = 4;  // waves of a workgroup
 
 // LDS of a workgroup.
@@ -293,7 +302,8 @@ struct PackedLds {
   float ml[NW][32][2];
 };
 
-// A tile of 128 rows of one sequence against all its keys: four waves of 32 rows.
+// A tile of 128 rows of one sequence against its keys or a part of them: four waves of 32
+// rows.
 template <int D>
 __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds) {
   constexpr int BLK = 32 * NW, BK = 32;
@@ -311,6 +321,7 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
   float l_run = 0.f;      // this lane's share of the row sum
   int hidden;             // keys of the unit that some row does not see, if > 0
   int used;               // rows of the sequence from this wave's first on
+  bool partial;           // not all of the sequence's keys: the result is joined later
   {
     const int lane = threadIdx.x & 63;
     const int g = lane >> 5;
@@ -346,7 +357,9 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
     }
     const RowAt at = row_at(a, it, w * 32 + (lane & 31));
     const Row<D> row = row_of<D>(a, it, at, kvh, g);
-    if (g == 0) out[w * 32 + lane] = row_out(a, it, at, kvh);
+    partial = it.part >= 0;
+    if (g == 0)
+      out[w * 32 + lane] = partial ? part_out<D>(a, it, w * 32 + lane, kvh) : row_out(a, it, at, kvh);
     used = it.rows - w * 32;
     const int left = row.left;
     const int whole = seen_from(a, it, w * 32);  // keys every row of the wave sees
@@ -480,6 +493,22 @@ __device__ __forceinline__ void tile_unit(const PackedArgs& a, PackedLds<D>& lds
 
   const PackedArgs b = late_args();
   const float l_tot = add_partner(l_run);
+  if (partial) {
+    if (er >= used) return;
+    const RowOut to = out[w * 32 + er];
+    float* const po = b.part_o + to.at + 4 * eg;
+#pragma unroll
+    for (int db = 0; db < C::DB; ++db)
+#pragma unroll
+      for (int qd = 0; qd < 4; ++qd) {
+        f32x4_t v;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = oacc[db][qd * 4 + u];
+        *reinterpret_cast<f32x4_t*>(po + db * 32 + qd * 8) = v;
+      }
+    if (eg == 0) *reinterpret_cast<f32x2_t*>(b.part_ml + to.lse) = f32x2_t{m_run, l_tot};
+    return;
+  }
   const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
   // O leaves through this wave's part of the K ring, which no wave reads any more, so
   // that a store instruction writes whole rows
@@ -699,37 +728,29 @@ __global__ void __launch_bounds__(64 * NW)
     few_unit<D>(a, lds);
 }
 
-// Rows whose keys were split: one workgroup per row and key head.  Wave w takes parts w,
-// w + 8, ... (lane t the max and sum of its t-th), rescales their outputs to the wave's
-// max and adds them in order; the waves' states are then merged in order.  The outputs'
-// loads do not wait for the weights.
+// Rows whose keys were split: up to kFewParts parts a wave per row and key head, more
+// (plan order: first) a workgroup, whose wave w takes parts w, w + 8, ... and whose states
+// are then merged in order.  Lane t holds the max and sum of the wave's t-th part; the
+// outputs, rescaled to the wave's max, are added in order, and their loads do not wait
+// for the weights.
 constexpr int kJoinWaves = 8;
-constexpr int kJoinMost = kMostParts / kJoinWaves;  // parts of a wave
+static_assert(kMostParts / kJoinWaves <= 64 && kFewParts <= 64, "a lane for each part of a wave");
 
-template <typename T, int D>
-__global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(const PackedArgs a) {
+// o (un-normalised), max and sum of parts at(0) .. at(n - 1); m, f: see above.
+template <int D, typename At>
+__device__ __forceinline__ float join_wave(const PackedArgs& a, At&& at, int n, int lane, float& m,
+                                           float* acc) {
   constexpr int PL = D / 64;  // values per lane
-  __shared__ float ml[kJoinWaves][2];
-  __shared__ float opart[kJoinWaves][D];
-  const int unit = divide((int)blockIdx.x, a.by_H_kv);
-  const int kvh = (int)blockIdx.x - unit * a.H_kv;
-  const PackedJoin j = a.joins[unit];
-  if (!inside(a, j)) return;
-  const int lane = threadIdx.x & 63;
-  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  auto at = [&](int i) { return (int64_t)(j.part + (int64_t)i * j.step) * a.H_kv + kvh; };
-  int n = (j.n - w + kJoinWaves - 1) / kJoinWaves;  // parts of this wave
-  static_assert(kJoinMost <= 64, "a lane for each part of a wave");
+  constexpr int U = 8;        // outputs in flight
   f32x2_t mine = {kNegBig, 0.f};
-  if (lane < n) mine = *reinterpret_cast<const f32x2_t*>(a.part_ml + 2 * at(w + kJoinWaves * lane));
-  float acc[PL] = {};
-  float m = kNegBig, f = 0.f;
-  constexpr int U = 8;  // outputs in flight
+  if (lane < n) mine = *reinterpret_cast<const f32x2_t*>(a.part_ml + 2 * at(lane));
+  m = kNegBig;
+  float f = 0.f;
   for (int t0 = 0; t0 < n; t0 += U) {
     float po[U][PL];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const float* p = a.part_o + at(w + kJoinWaves * (t0 + u < n ? t0 + u : 0)) * D + lane * PL;
+      const float* p = a.part_o + at(t0 + u < n ? t0 + u : 0) * D + lane * PL;
 #pragma unroll
       for (int e = 0; e < PL; ++e) po[u][e] = p[e];
     }
@@ -748,7 +769,44 @@ __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(const PackedArgs 
       }
     }
   }
-  const float lw = wave_sum(f * mine[1]);
+  return wave_sum(f * mine[1]);
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(const PackedArgs a) {
+  constexpr int PL = D / 64;
+  __shared__ float ml[kJoinWaves][2];
+  __shared__ float opart[kJoinWaves][D];
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wide = a.n_wide * a.H_kv;  // rows with a workgroup each
+  const bool own = (int)blockIdx.x >= wide;
+  const int64_t x = own ? wide + ((int64_t)blockIdx.x - wide) * kJoinWaves + w : blockIdx.x;
+  if (x >= (int64_t)a.n_joins * a.H_kv) return;  // (a whole wave of a workgroup without a barrier)
+  const int unit = divide((int)x, a.by_H_kv);
+  const int kvh = (int)x - unit * a.H_kv;
+  const PackedJoin j = a.joins[unit];
+  if (!inside(a, j) || (own && j.n > kFewParts)) return;
+  const int64_t head = kvh * a.G + j.in_group;
+  T* const op = static_cast<T*>(a.o) + j.q_row * a.ot + head * a.oh;
+  float acc[PL] = {}, m;
+  auto finish = [&](float l) {
+    if (a.lse != nullptr && lane == 0 && (own || w == 0))
+      a.lse[head * a.lse_head + j.q_row] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
+    return l == 0.f ? 0.f : 1.0f / l;
+  };
+  if (own) {
+    const float l = join_wave<D>(
+        a, [&](int i) { return (int64_t)(j.part + (int64_t)i * j.step) * a.H_kv + kvh; }, j.n, lane, m, acc);
+    const float inv = finish(l);
+#pragma unroll
+    for (int e = 0; e < PL; ++e) op[lane * PL + e] = (T)(acc[e] * inv);
+    return;
+  }
+  const float lw = join_wave<D>(
+      a,
+      [&](int i) { return (int64_t)(j.part + (int64_t)(w + kJoinWaves * i) * j.step) * a.H_kv + kvh; },
+      (j.n - w + kJoinWaves - 1) / kJoinWaves, lane, m, acc);
   if (lane == 0) {
     ml[w][0] = m;
     ml[w][1] = lw;
@@ -758,23 +816,20 @@ __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(const PackedArgs 
   __syncthreads();
   m = kNegBig;
 #pragma unroll
-  for (int x = 0; x < kJoinWaves; ++x) m = fmaxf(m, ml[x][0]);
+  for (int y = 0; y < kJoinWaves; ++y) m = fmaxf(m, ml[y][0]);
   float l = 0.f, wgt[kJoinWaves];
 #pragma unroll
-  for (int x = 0; x < kJoinWaves; ++x) {
-    wgt[x] = fast_exp2(ml[x][0] - m);
-    l = __builtin_fmaf(ml[x][1], wgt[x], l);
+  for (int y = 0; y < kJoinWaves; ++y) {
+    wgt[y] = fast_exp2(ml[y][0] - m);
+    l = __builtin_fmaf(ml[y][1], wgt[y], l);
   }
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  const int64_t head = kvh * a.G + j.in_group;
+  const float inv = finish(l);
   for (int e = threadIdx.x; e < D; e += 64 * kJoinWaves) {
     float o = 0.f;
 #pragma unroll
-    for (int x = 0; x < kJoinWaves; ++x) o = __builtin_fmaf(opart[x][e], wgt[x], o);
-    static_cast<T*>(a.o)[j.q_row * a.ot + head * a.oh + e] = (T)(o * inv);
+    for (int y = 0; y < kJoinWaves; ++y) o = __builtin_fmaf(opart[y][e], wgt[y], o);
+    op[e] = (T)(o * inv);
   }
-  if (a.lse != nullptr && threadIdx.x == 0)
-    a.lse[head * a.lse_head + j.q_row] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
 template <int D, int KINDS>
@@ -811,10 +866,11 @@ hipError_t launch_packed_bf16(int d, const PackedArgs& a, int n_few, hipStream_t
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_packed_join(int d, bool bf16, const PackedArgs& a, int n_joins,
-                              hipStream_t stream) {
-  if (n_joins == 0) return hipSuccess;
-  const dim3 grid((uint32_t)n_joins * a.H_kv), block(64 * kJoinWaves);
+hipError_t launch_packed_join(int d, bool bf16, const PackedArgs& a, hipStream_t stream) {
+  if (a.n_joins == 0) return hipSuccess;
+  const int64_t own = (int64_t)(a.n_joins - a.n_wide) * a.H_kv;
+  const dim3 grid((uint32_t)(a.n_wide * a.H_kv + (own + kJoinWaves - 1) / kJoinWaves)),
+      block(64 * kJoinWaves);
   if (bf16 && d == 64)
     hipLaunchKernelGGL((join_kernel<__bf16, 64>), grid, block, 0, stream, a);
   else if (bf16 && d == 128)

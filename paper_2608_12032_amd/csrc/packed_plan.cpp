@@ -21,13 +21,37 @@ int part_keys(bool bf16, int k_len) {
   return (int)(keys < least ? least : keys);
 }
 
+// Keys of a part of a sequence whose rows fill up to 16 tiles: all of them, but where they
+// are many (a chunk of a prompt, drafted tokens, over a long cache), a walk that would
+// leave most CUs idle.  A part costs its rows' partial results once more, written and
+// read: the more rows, the more keys it takes.  us, whole / split, one sequence and eight
+// (fp32 four), causal, d = 128:
+//   bf16, 32 / 4 heads, 7 tokens over 4,096 keys 65 / 17, 66 / 22; 32,768 470 / 27, 479 / 121
+//   32 / 8 heads, 256 tokens over 4,096 keys 68 / 49, 124 / 158; 32,768 488 / 161, 977 / 1,026
+//   512 tokens over 32,768 keys 490 / 281, 1,920 / 1,998
+//   fp32, 12 / 4 heads, 64 tokens over 2,048 keys 45 / 24, 50 / 53; 32,768 570 / 142, 658 / 464
+// and with 512 keys a part at least 256 tokens over 4,096 keys took 58 and 412, over 2,048 42
+// and 253 (whole 38 and 66).
+constexpr int kSplitTiles = 16;
+int tile_part_keys(bool bf16, int64_t rows, int k_len) {
+  const int block = kPackedTile[bf16];
+  const int64_t tiles = (rows + block - 1) / block;
+  if (tiles > kSplitTiles) return k_len;
+  const bool many = tiles > kSplitTiles / 2;
+  const int least = !bf16 ? (many ? 1024 : 512) : rows <= block / 2 ? 512 : many ? 8192 : 2048;
+  const int parts = std::min(k_len / least, (bf16 ? 32 : 64) / (int)tiles);
+  if (parts < 2) return k_len;
+  const int step = bf16 ? 64 : 256;  // whole rounds of a workgroup's sub-tiles
+  return ((k_len + parts - 1) / parts + step - 1) / step * step;
+}
+
 // fp32 units of 32 rows below which a call takes 16.  us in tiles of 16 / of 32, dense:
 // 128 units (1,024 x 4 heads, d = 128) 25.6 / 39.7; 256 47.2 / 40.2 and causal 31.7 / 40.2;
 // 555 410 / 427, at d = 64 200 / 232; 768 255 / 211, at d = 64 119 / 116.
 constexpr int64_t kWideUnits = 640;
 
 struct Counts {
-  int64_t tiles, few, joins, part_rows;
+  int64_t tiles, few, joins, wide, part_rows;
 };
 
 // Rows of a call's tiles.  fp32: 16 where tiles of 32 would make few rounds of the
@@ -37,7 +61,9 @@ int tile_rows(const PackedSeqs& s) {
   int64_t wide = 0;
   for (int i = 0; i < s.n; ++i) {
     const int64_t rows = (int64_t)s.q_len[i] * s.G;
-    if (rows > kPackedFew[0]) wide += (rows + kPackedTile[0] - 1) / kPackedTile[0];
+    if (rows <= kPackedFew[0]) continue;
+    const int keys = std::max(1, tile_part_keys(false, rows, s.k_len[i]));
+    wide += (rows + kPackedTile[0] - 1) / kPackedTile[0] * std::max(1, (s.k_len[i] + keys - 1) / keys);
   }
   return wide * s.H_kv < kWideUnits ? kPackedNarrow : kPackedTile[0];
 }
@@ -45,7 +71,7 @@ int tile_rows(const PackedSeqs& s) {
 // Calls tile(item), few(item), join(row) for every unit, in order; returns their number.
 template <typename Tile, typename Few, typename Join>
 Counts walk(const PackedSeqs& s, int block, Tile&& tile, Few&& few, Join&& join) {
-  Counts c = {0, 0, 0, 0};
+  Counts c = {};
   int64_t q0 = 0, k0 = 0;
   for (int i = 0; i < s.n; ++i) {
     const int64_t q_start = s.q_start ? s.q_start[i] : q0, k_start = s.k_start ? s.k_start[i] : k0;
@@ -57,42 +83,49 @@ Counts walk(const PackedSeqs& s, int block, Tile&& tile, Few&& few, Join&& join)
     if (rows == 0) continue;
     PackedItem it = {};
     it.part = -1;
-    if (rows > kPackedFew[s.bf16]) {
+    const bool tiled = rows > kPackedFew[s.bf16];
+    const int keys = tiled ? tile_part_keys(s.bf16, rows, k_len) : part_keys(s.bf16, k_len);
+    const int parts = std::max(1, (int)(((int64_t)k_len + keys - 1) / std::max(1, keys)));
+    if (tiled) {
       for (int64_t r = 0; r < rows; r += block) {
         const int tok = (int)(r / s.G);
         const int last = (int)std::min<int64_t>(q_len - 1, (r + block - 1) / s.G);
         it.q_row = q_start + tok;
         it.head0 = (int)(r - (int64_t)tok * s.G);
         it.rows = (int)(rows - r);
-        it.keys = s.causal ? std::max(0, std::min(k_len, last + shift + 1)) : k_len;
-        it.seen = s.causal ? tok + shift + 1 : kAllSeen;
-        it.k_row = it.keys > 0 ? k_start : 0;
-        tile(it);
-        ++c.tiles;
+        const int seen = s.causal ? std::max(0, std::min(k_len, last + shift + 1)) : k_len;
+        for (int p = 0; p < parts; ++p) {
+          const int first = p * keys;
+          it.keys = std::max(0, std::min(seen - first, keys));
+          it.k_row = it.keys > 0 ? k_start + first : 0;
+          it.seen = s.causal ? tok + shift + 1 - first : kAllSeen;
+          if (parts > 1) it.part = (int)(c.part_rows + p * rows + r);
+          tile(it);
+          ++c.tiles;
+        }
       }
-      continue;
-    }
-    const int keys = part_keys(s.bf16, k_len);
-    const int parts = std::max(1, (int)(((int64_t)k_len + keys - 1) / keys));
-    it.q_row = q_start;
-    it.rows = (int)rows;
-    for (int p = 0; p < parts; ++p) {
-      const int first = p * keys;
-      it.keys = std::min(k_len - first, keys);
-      it.k_row = it.keys > 0 ? k_start + first : 0;
-      it.seen = s.causal ? shift + 1 - first : kAllSeen;
-      if (parts > 1) it.part = (int)(c.part_rows + p * rows);
-      few(it);
-      ++c.few;
+    } else {
+      it.q_row = q_start;
+      it.rows = (int)rows;
+      for (int p = 0; p < parts; ++p) {
+        const int first = p * keys;
+        it.keys = std::min(k_len - first, keys);
+        it.k_row = it.keys > 0 ? k_start + first : 0;
+        it.seen = s.causal ? shift + 1 - first : kAllSeen;
+        if (parts > 1) it.part = (int)(c.part_rows + p * rows);
+        few(it);
+        ++c.few;
+      }
     }
     if (parts > 1) {
       for (int64_t r = 0; r < rows; ++r) {
         join(PackedJoin{q_start + r / s.G, (int)(r % s.G), (int)(c.part_rows + r), (int)rows, parts});
         ++c.joins;
+        c.wide += parts > kFewParts;
       }
       c.part_rows += parts * rows;
-      if (c.part_rows >= ((int64_t)1 << 31)) break;
     }
+    if (std::max(c.tiles + c.few, c.part_rows) >= ((int64_t)1 << 31)) break;  // too many
   }
   return c;
 }
@@ -109,6 +142,7 @@ bool packed_counts(const PackedSeqs& s, PackedCounts* out) {
   out->tiles = (int)c.tiles;
   out->few = (int)c.few;
   out->joins = (int)c.joins;
+  out->wide = (int)c.wide;
   out->part_rows = c.part_rows;
   return true;
 }
@@ -117,9 +151,9 @@ void packed_fill(const PackedSeqs& s, const PackedCounts& n, void* plan) {
   PackedItem* const tiles = static_cast<PackedItem*>(plan);
   PackedItem* const few = tiles + n.tiles;
   PackedJoin* const joins = reinterpret_cast<PackedJoin*>(few + n.few);
-  int64_t t = 0, f = 0, j = 0;
+  int64_t t = 0, f = 0, j[2] = {n.wide, 0};
   walk(s, n.tile_rows, [&](const PackedItem& x) { tiles[t++] = x; }, [&](const PackedItem& x) { few[f++] = x; },
-       [&](const PackedJoin& x) { joins[j++] = x; });
+       [&](const PackedJoin& x) { joins[j[x.n > kFewParts]++] = x; });
   // longest first, so that the launch's tail is made of short units; order changes only
   // the schedule.  (std::sort: no allocation)
   auto longer = [](const PackedItem& a, const PackedItem& b) {

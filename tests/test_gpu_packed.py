@@ -91,10 +91,14 @@ CASES = [  # dtype, d, H, Hkv, causal, q_lens, k_lens
     (BF, 64, 4, 4, True, (1, 2, 7, 32, 5, 1, 3), (5000, 300, 1000, 700, 3, 0, 1)),
     (BF, 128, 24, 1, False, (1, 1, 1), (513, 7000, 64)), (BF, 128, 96, 3, True, (1, 1), (900, 31)),
     (BF, 64, 5, 1, False, (6, 1), (20_000, 70_000)),
+    # tiles whose keys are split: drafted tokens and chunks over a cache
+    (BF, 128, 8, 1, True, (7, 5, 33, 16), (9000, 2048, 4111, 2047)),
+    (BF, 64, 8, 2, True, (100, 9, 256), (6000, 20_003, 2600)), (BF, 128, 6, 2, False, (43, 11), (2049, 30_000)),
     # mixed
     (BF, 128, 4, 2, True, (0, 1, 600, 3, 0, 17, 64), (4, 900, 600, 3, 0, 2100, 64)),
     (F, 128, 2, 2, False, (1, 15, 16, 17, 31, 32, 33, 150), (1, 31, 32, 33, 255, 256, 257, 300)),
     (F, 64, 6, 2, True, (100, 1, 333, 64), None), (F, 128, 3, 1, True, (40, 130), (300, 60)),
+    (F, 128, 4, 1, True, (20, 5, 64), (3001, 9000, 2048)), (F, 64, 3, 1, False, (90, 6), (2050, 7000)),
     (F, 64, 8, 2, True, (1, 4, 2, 1), (3000, 511, 513, 20_011)),
     (F, 128, 4, 4, True, (1, 16, 3, 0, 9), (0, 2000, 2, 5, 1100)),
     (F, 128, 32, 2, False, (1, 1), (700, 5000)),
@@ -250,6 +254,35 @@ def test_what_a_row_does_not_see_does_not_reach_it(L, dtype, bad):
             if which == 0 and first < ql[i]:  # and rows that see one are not finite
                 seen = o[ends_q[i] + max(0, first):ends_q[i + 1]]
                 assert not torch.isfinite(seen).any()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_tiles_over_a_long_cache(L, dtype):
+    """Rows of tiles whose keys are split: the same bits alone and packed, values that are
+    not finite at keys that a row does not see."""
+    d, ql, kl = 64, (90, 40, 300, 2600), (5000, 2500, 700, 2300)
+    q = randn(sum(ql), 4, d, seed=70, dtype=dtype).cuda()
+    k, v = (randn(sum(kl), 2, d, seed=s, dtype=dtype).cuda() for s in (71, 72))
+    o, lse = call(L, q, k, v, ql, kl, True)
+    a = b = 0
+    for x, y in zip(ql, kl):
+        o1, l1 = call(L, q[a:a + x], k[b:b + y], v[b:b + y], [x], [y], True)
+        assert torch.equal(o1, o[a:a + x]) and torch.equal(l1, lse[:, a:a + x])
+        a, b = a + x, b + y
+    ref = reference(q[:90], k[:5000], v[:5000], True, d ** -0.5)
+    check(o[:90], lse[:, :90], ref, 5000, d)
+    for cut in (4915, 4950, 4999):
+        v2 = v.clone()
+        v2[cut:5000] = float("nan")
+        k2 = k.clone()
+        k2[cut:5000] = float("inf")
+        n = cut - 4910  # rows that see no key from `cut` on
+        o2, l2 = call(L, q, k2, v2, ql, kl, True)
+        check(o2[:n], l2[:, :n], tuple(x[:n] if x.dim() == 3 else x[:, :n] for x in ref), 5000, d)
+        assert not torch.isfinite(o2[n:90]).any() and torch.equal(o2[90:], o[90:])
+    for keys in (2048, 130):  # the fewest that are split; rows that see nothing
+        o, lse = call(L, q[:256], k[:keys], v[:keys], [256], [keys], True)
+        check(o, lse, reference(q[:256], k[:keys], v[:keys], True, d ** -0.5), keys, d)
 
 
 @pytest.mark.parametrize("dtype", [BF, F])

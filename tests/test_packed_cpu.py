@@ -62,28 +62,34 @@ def test_units_cover_every_row_and_key_once(L, dtype, causal, seed):
                 tok = int(x["q_row"]) - q0 + t
                 assert max(0, min(int(x["keys"]), int(x["seen"]) + t)) == \
                     max(0, min(c0 + int(x["keys"]), sees(tok)) - c0)
-        if rows > most:
-            assert sorted(map(number, mine)) == list(range(0, rows, block))
-            for x in mine:
-                last = min(q - 1, (number(x) + block - 1) // G)
-                assert x["part"] == -1 and x["keys"] == sees(last)
-                assert x["keys"] == 0 or x["k_row"] == k0
-        elif rows:
-            mine = sorted(mine, key=lambda x: x["k_row"])
-            assert all(number(x) == 0 for x in mine) and sum(int(x["keys"]) for x in mine) == k
-            assert len(mine) <= 256 and (k == 0 or mine[0]["k_row"] == k0)
-            assert all(a["k_row"] + a["keys"] == b["k_row"] for a, b in zip(mine, mine[1:]))
-            if len(mine) == 1:
-                assert mine[0]["part"] == -1
+        # a tile's or a few-row sequence's keys, part after part
+        by_row = {}
+        for x in mine:
+            by_row.setdefault(number(x), []).append(x)
+        assert sorted(by_row) == (list(range(0, rows, block)) if rows > most else [0][:rows])
+        n = firsts = None
+        for r, those in by_row.items():
+            those.sort(key=lambda x: x["part"])
+            last = min(q - 1, (r + block - 1) // G)
+            assert sum(int(x["keys"]) for x in those) == (sees(last) if rows > most else k)
+            held = [x for x in those if x["keys"]]
+            assert not held or held[0]["k_row"] == k0
+            assert all(a["k_row"] + a["keys"] == b["k_row"] for a, b in zip(held, held[1:]))
+            assert n in (None, len(those)) and len(those) <= 256
+            n = len(those)
+            if n == 1:
+                assert those[0]["part"] == -1
             else:
-                first = int(mine[0]["part"])
-                assert [int(x["part"]) for x in mine] == [first + i * rows for i in range(len(mine))]
-                got = [j for j in joins if q0 <= j["q_row"] < q0 + q]
-                assert sorted((int(j["q_row"]) - q0) * G + int(j["in_group"]) for j in got) == list(range(rows))
-                for j in got:
-                    r = (int(j["q_row"]) - q0) * G + int(j["in_group"])
-                    assert (j["part"], j["step"], j["n"]) == (first + r, rows, len(mine))
-                parts.append((first, first + len(mine) * rows))
+                at = [int(x["part"]) - r for x in those]
+                assert firsts in (None, at[0]) and at == [at[0] + i * rows for i in range(n)]
+                firsts = at[0]
+        if n is not None and n > 1:
+            got = [j for j in joins if q0 <= j["q_row"] < q0 + q]
+            assert sorted((int(j["q_row"]) - q0) * G + int(j["in_group"]) for j in got) == list(range(rows))
+            for j in got:
+                r = (int(j["q_row"]) - q0) * G + int(j["in_group"])
+                assert (j["part"], j["step"], j["n"]) == (firsts + r, rows, n)
+            parts.append((firsts, firsts + n * rows))
         q0, k0 = q0 + q, k0 + k
     parts.sort()
     assert sum(b - a for a, b in parts) == p.info.part_rows
