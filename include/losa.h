@@ -292,7 +292,8 @@ losa_status losa_construct(const void* q, const void* k, const void* v, losa_dty
 /* Rows of `d` contiguous elements at data + b*batch + n*token + h*head (strides in
    elements; b < B, n < N, h < H).  data 16-byte aligned, strides multiples of 16
    bytes and >= 0.  An input may have stride 0 (a broadcast view); the rows of an
-   output must not overlap. */
+   output must not overlap (losa_rope and losa_qk_norm_rope: each axis steps over all
+   that the axes of smaller strides span). */
 typedef struct {
   void* data;
   int64_t batch, token, head;

@@ -155,6 +155,8 @@ losa_status losa_packed_attn_fwd(const losa_view* q, const losa_view* k, const l
     if (workspace_bytes < need)
       return fail(LOSA_ERR_CAPACITY, "workspace_bytes=%zu < %zu", workspace_bytes, need);
   }
+  if ((ov.data == qv.data && !losa::same_rows(ov, qv)) || ov.data == kv[0].data || ov.data == kv[1].data)
+    return fail(LOSA_ERR_INVALID_SHAPE, "o may lie over q only as the same view, and not over k or v");
   losa::PackedArgs a = {};
   a.items = static_cast<const losa::PackedItem*>(plan);
   a.joins = reinterpret_cast<const losa::PackedJoin*>(a.items + info->n_tiles + info->n_few);

@@ -2,6 +2,7 @@
 // table, argument checks, dispatch.
 #include "losa.h"
 
+#include <algorithm>
 #include <cmath>
 
 #include "abi.hpp"
@@ -30,12 +31,17 @@ losa_status losa::take_view(const char* name, const losa_view* from, losa_view* 
   return LOSA_OK;
 }
 
+bool losa::same_rows(const losa_view& a, const losa_view& b) {
+  return a.data == b.data && a.batch == b.batch && a.token == b.token && a.head == b.head;
+}
+
 namespace {
 
 using losa::aligned16;
 using losa::elem_bytes;
 using losa::fail;
 using losa::hip_status;
+using losa::same_rows;
 using losa::take_view;
 
 losa_status check_rows(losa_dtype dtype, int B, int N, int N_pad, int H, int d) {
@@ -48,6 +54,23 @@ losa_status check_rows(losa_dtype dtype, int B, int N, int N_pad, int H, int d) 
     return fail(LOSA_ERR_UNSUPPORTED, "unknown dtype %d", (int)dtype);
   if (d != 64 && d != 128)
     return fail(LOSA_ERR_UNSUPPORTED, "head dim d=%d not supported (64 or 128)", d);
+  return LOSA_OK;
+}
+
+// Rows of an output: an axis steps over all that those of smaller strides span, as in any
+// slice or permutation of a contiguous tensor.
+losa_status check_spread(const char* name, const losa_view& y, int B, int N, int H, int d) {
+  const int64_t stride[3] = {y.batch, y.token, y.head}, n[3] = {B, N, H};
+  int by[3] = {0, 1, 2};
+  std::sort(by, by + 3, [&](int i, int j) { return stride[i] < stride[j]; });
+  __int128 span = d;
+  for (int i : by) {
+    if (n[i] <= 1) continue;
+    if (stride[i] < span)
+      return fail(LOSA_ERR_INVALID_SHAPE, "%s: rows of an output overlap (stride %lld)", name,
+                  (long long)stride[i]);
+    span += (__int128)stride[i] * (n[i] - 1);
+  }
   return LOSA_OK;
 }
 
@@ -111,6 +134,20 @@ losa_status rows_status(hipError_t e, const char* what) {
   return hip_status(e, what);
 }
 
+// Outputs that start where another tensor of the call does: only an output over its own
+// input, row for row.  (Views that overlap elsewhere are the caller's to avoid.)
+losa_status check_apart(const losa_view* in, const losa_view* out, int n, bool padded) {
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < n; ++j) {
+      if (out[i].data == in[j].data && (i != j || padded || !same_rows(out[i], in[j])))
+        return fail(LOSA_ERR_INVALID_SHAPE,
+                    "an output may lie over its own input only as the same view, with N_pad = N");
+      if (i != j && out[i].data == out[j].data)
+        return fail(LOSA_ERR_INVALID_SHAPE, "two outputs lie over each other");
+    }
+  return LOSA_OK;
+}
+
 void set_tensor(losa::RowsTensor* t, const losa_view& x, const losa_view& y, int H) {
   t->x = x.data;
   t->xb = x.batch;
@@ -159,8 +196,10 @@ losa_status losa_rope(const losa_view* x, losa_dtype dtype, int B, int N, int N_
   losa_view xv, yv;
   if ((st = take_view("x", x, &xv, el, B, N, H, d, false)) != LOSA_OK) return st;
   if ((st = take_view("y", y, &yv, el, B, N_pad, H, d, true)) != LOSA_OK) return st;
+  if ((st = check_spread("y", yv, B, N_pad, H, d)) != LOSA_OK) return st;
   losa::RowsArgs a = {};
   if ((st = check_rotation(rot, N, d, &a)) != LOSA_OK) return st;
+  if ((st = check_apart(&xv, &yv, 1, N_pad != N)) != LOSA_OK) return st;
   a.B = B;
   a.N = N;
   a.n_pad = N_pad;
@@ -186,11 +225,14 @@ losa_status losa_qk_norm_rope(const losa_view* q, const losa_view* k, const losa
   if ((st = take_view("k", k, &in[1], el, B, N, H_kv, d, false)) != LOSA_OK) return st;
   if ((st = take_view("q_out", q_out, &to[0], el, B, N_pad, H, d, true)) != LOSA_OK) return st;
   if ((st = take_view("k_out", k_out, &to[1], el, B, N_pad, H_kv, d, true)) != LOSA_OK) return st;
+  if ((st = check_spread("q_out", to[0], B, N_pad, H, d)) != LOSA_OK) return st;
+  if ((st = check_spread("k_out", to[1], B, N_pad, H_kv, d)) != LOSA_OK) return st;
   if ((v == nullptr) != (v_out == nullptr))
     return fail(LOSA_ERR_NULL_POINTER, "v and v_out must both be given or both be NULL");
   if (v) {
     if ((st = take_view("v", v, &in[2], el, B, N, H_kv, d, false)) != LOSA_OK) return st;
     if ((st = take_view("v_out", v_out, &to[2], el, B, N_pad, H_kv, d, true)) != LOSA_OK) return st;
+    if ((st = check_spread("v_out", to[2], B, N_pad, H_kv, d)) != LOSA_OK) return st;
   }
   losa::RowsArgs a = {};
   if (rot && (st = check_rotation(rot, N, d, &a)) != LOSA_OK) return st;
@@ -205,6 +247,7 @@ losa_status losa_qk_norm_rope(const losa_view* q, const losa_view* k, const losa
       return fail(LOSA_ERR_ALIGNMENT, "norm weights and biases must be 16-byte aligned");
     all = norm->all_heads != 0;
   }
+  if ((st = check_apart(in, to, v ? 3 : 2, N_pad != N)) != LOSA_OK) return st;
   a.B = B;
   a.N = N;
   a.n_pad = N_pad;

@@ -520,7 +520,8 @@ def losa_rope(x, table: RopeTable, pos, n_pad: int | None = None, pairing: str =
               out=None):
     """Rotary positions of x [B, N, H, d] (any strides, rows of d contiguous) ->
     [B, H, n_pad, d], rows from N on 0.  ``pos`` int32 [axes, N] or [B, axes, N];
-    ``out`` may have any strides, and may be x's own memory."""
+    ``out`` may have any strides, and may be x itself
+    (x.transpose(1, 2) with n_pad = N)."""
     shape = B, N, H, d = _rows_in(x, "x")
     n_pad = N if n_pad is None else n_pad
     dev, dt, code = x.device, x.dtype, _dtype_code(x)

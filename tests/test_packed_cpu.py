@@ -198,6 +198,13 @@ def test_forward_stride_refusals(L):
         assert fwd(L, **{which: view(L, token=(1 << 25) + 8)}) == 2
 
 
+def test_an_output_over_other_tensors_is_refused(L):
+    at = [view(L, data=FAKE + (i << 24)) for i in range(4)]
+    args = dict(zip("qkvo", at))
+    for kw in (dict(o=view(L, data=at[0].data, token=128, head=5120)), dict(o=at[1]), dict(o=at[2])):
+        assert fwd(L, **{**args, **kw}) == 2 and "may lie over" in L.lib.losa_last_error().decode()
+
+
 def test_forward_refuses_what_is_no_info(L):
     info = L.losa_packed_plan([4], [300], 4, 2, torch.bfloat16, device="cpu").info
     for name, value in (("H", 5), ("H_kv", 0), ("n_tiles", 3), ("bytes", 8), ("dtype", 4), ("n_few", -1), ("tile_rows", 64)):

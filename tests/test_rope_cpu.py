@@ -136,6 +136,31 @@ def test_overlapping_output_rows_are_refused(L, kw):
     assert rope(L, y=view(L, **kw)) == 2
 
 
+@pytest.mark.parametrize("kw", [
+    dict(token=128, head=256),          # heads of one token over those of the next
+    dict(batch=99 * 512 + 384), dict(token=512, head=256, batch=100 * 512),
+    dict(token=1 << 39, head=1 << 39, batch=1 << 39)])
+def test_rows_that_step_into_each_other_are_refused(L, kw):
+    assert rope(L, y=view(L, **kw)) == 2
+    assert "overlap" in L.lib.losa_last_error().decode()
+
+
+def test_outputs_over_other_tensors_are_refused(L):
+    """An output may be its own input, the same view; nothing else starts where it does."""
+    head_major = dict(batch=100 * 512, token=128, head=100 * 128)
+    assert rope(L, y=view(L, **head_major)) == 2 and "same view" in L.lib.losa_last_error().decode()
+    assert rope(L, N_pad=128, x=view(L, batch=128 * 512), y=view(L, batch=128 * 512)) == 2
+    at = [view(L, data=FAKE + (i << 24)) for i in range(6)]
+    for kw in (dict(qo=at[1]), dict(ko=at[0]), dict(vo=at[1]), dict(qo=at[4]), dict(ko=at[5]),
+               dict(vo=view(L, data=at[2].data, **head_major)), dict(vo=at[2], N_pad=128)):
+        n_pad = kw.get("N_pad", 100)
+        t = dict(zip(("q", "k", "v", "qo", "ko", "vo"), at))
+        if n_pad == 128:
+            t = {x: View(y.data, 128 * 512, y.token, y.head) for x, y in t.items()}
+        t.update(kw)
+        assert qkn(L, **t) == 2, kw
+
+
 def norms(L, kind=1, all_heads=0, eps=1e-6, qw=None, qb=None, kw=None, kb=None):
     return QkNorm(kind, all_heads, eps, qw, qb, kw, kb)
 
