@@ -3,7 +3,8 @@
  * ("Near-Lossless Sparse Attention for Training-Free Video Diffusion
  * Acceleration"): exact block masses at the construction step, the
  * shortest-prefix block selection, and block-sparse attention over the frozen
- * support.
+ * support.  Around the path: rotary positions, norms of queries and keys, and
+ * attention over packed sequences.
  *
  * Conventions shared by every call
  * --------------------------------
@@ -12,7 +13,7 @@
  *   keeps no state between calls except a thread-local error string, and for
  *   losa_sparse_attn_fwd_noalloc a scratch array per GPU (reserved when the
  *   library's code is loaded on that GPU) with a table of its addresses.
- * - Q, K, V, O are contiguous [B][H][N_pad][d] in the element type `dtype`,
+ * - Q, K, V, O of the path are contiguous [B][H][N_pad][d] in the element type `dtype`,
  *   N_pad = N rounded up to max(block_q, block_k).  Token positions n >= N
  *   are padding: as keys they never enter a softmax; as queries they are left
  *   out of every block mass and their output rows are written as 0 (lse as
@@ -28,7 +29,8 @@
  *   only on `stream`, so calls can be captured into a HIP graph and replayed
  *   (tested for losa_construct, losa_select_blocks, losa_select_blocks_topk,
  *   losa_sparse_attn_fwd and both losa_calibrate_mass schemes, which also set
- *   their kernel's dynamic LDS size on the host).
+ *   their kernel's dynamic LDS size on the host, losa_rope, losa_qk_norm_rope and
+ *   losa_packed_attn_fwd).
  * - Validation is synchronous and happens before any HIP call: on an error
  *   nothing is launched, outputs are untouched, and losa_last_error() holds a
  *   description.  Launch failures return LOSA_ERR_HIP.
@@ -39,7 +41,7 @@
  * - Calls are deterministic: the same inputs give bitwise identical outputs, and
  *   a head gives the same bits alone and among other heads.
  * - Memory.  An output shares no memory with another output, the workspace or an
- *   input, except o with q (the same address), and bf16 o with v (anywhere).  An
+ *   input, except o with q (the same address), and bf16 o of the path with v (anywhere).  An
  *   o over k, or over v in f32, is not detected: rows still to come would read
  *   what finished rows have written.  f32 losa_construct uses o as scratch before
  *   it writes it (not where it overlaps an input).

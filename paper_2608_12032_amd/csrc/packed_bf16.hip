@@ -840,7 +840,7 @@ void launch_units(const PackedArgs& a, int units, hipStream_t stream) {
 }
 
 // Tiles of a call up to which both kinds share a launch at d = 128: it saves 3.4 us (10
-// prompts of 1 to 1,024 tokens x 32 / 8 heads, 246 x 8 tiles: 31.3 us, in two launches
+// prompts of 1 to 1,024 tokens x 32 / 8 heads, 120 x 8 units: 31.3 us, in two launches
 // 34.7), and the tiles are 2 % slower in it (12 heads x 8,192 dense: 370 / 361 us).  At
 // d = 64, where a kernel of both spills, they are 10 to 15 % slower.
 constexpr int64_t kTogether = 4096;

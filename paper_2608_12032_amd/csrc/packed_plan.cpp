@@ -30,8 +30,8 @@ int part_keys(bool bf16, int k_len) {
 //   32 / 8 heads, 256 tokens over 4,096 keys 68 / 49, 124 / 158; 32,768 488 / 161, 977 / 1,026
 //   512 tokens over 32,768 keys 490 / 281, 1,920 / 1,998
 //   fp32, 12 / 4 heads, 64 tokens over 2,048 keys 45 / 24, 50 / 53; 32,768 570 / 142, 658 / 464
-// and with 512 keys a part at least 256 tokens over 4,096 keys took 58 and 412, over 2,048 42
-// and 253 (whole 38 and 66).
+// and with 512 keys a part at least 256 tokens over 2,048 keys took 31 and 120 (whole 38
+// and 68).
 constexpr int kSplitTiles = 16;
 int tile_part_keys(bool bf16, int64_t rows, int k_len) {
   const int block = kPackedTile[bf16];
