@@ -21,7 +21,7 @@ struct PackedItem {
   int32_t keys;  // keys that some row of the unit sees
   int32_t seen;  // (kAllSeen: every row sees them all)
   int32_t part;  // first partial row to write, or -1: the result itself
-  int32_t unused;
+  int32_t split;  // fp32: 2^split waves of the workgroup share a row set
 };
 constexpr int32_t kAllSeen = 1 << 30;
 // One row whose keys were split: n partial rows at part, part + step, ...
@@ -79,11 +79,12 @@ __device__ __forceinline__ bool inside(const PackedArgs& a, const PackedJoin& j)
          (j.part + (int64_t)(j.n - 1) * j.step < a.part_rows);
 }
 
-// Rows of a tile (fp32: of a wide one; a call of few units takes tiles of 16), rows of
+// Rows of a tile (fp32: of a wide row set; a call of few units takes sets of 16), rows of
 // a sequence that make it a few-row one.
 constexpr int kPackedTile[2] = {32, 128};  // [bf16]
 constexpr int kPackedFew[2] = {16, 32};
 constexpr int kPackedNarrow = 16;
+constexpr int kPackedF32Waves = 8;
 // The sequences of a call as the plan takes them (starts null: one after another).
 struct PackedSeqs {
   const int64_t *q_start, *k_start;

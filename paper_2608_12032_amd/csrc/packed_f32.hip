@@ -1,8 +1,9 @@
 // Attention over packed sequences, fp32 inputs, on the fp32 matrix instructions: the
 // mathematics, units and plan of packed_bf16.hip with the tiles of the fp32 path
-// (f32_path.hip): a workgroup owns one or two groups of 16 rows, its eight waves take
-// the unit's 32-key sub-tiles in turn and merge their softmax states (max, sum in
-// fp64, O) in a fixed order through LDS.  K and V come straight to registers through
+// (f32_path.hip).  A wave takes one or two groups of 16 rows; the waves of a row set, all
+// eight of a workgroup or, over few keys, 4, 2 or 1 of them (packed_plan.cpp), take the
+// unit's 32-key sub-tiles in turn and merge their softmax states (max, sum in fp64, O)
+// in a fixed order through LDS.  K and V come straight to registers through
 // buffer resources of one sub-tile each, cut at the unit's last key: rows behind it
 // read as 0, and no offset passes 32 bits.
 //
@@ -19,7 +20,7 @@ namespace losa {
 
 namespace {
 
-constexpr int kWaves = 8;  // key splits of a workgroup: two waves per SIMD
+constexpr int kWaves = kPackedF32Waves;  // of a workgroup: two per SIMD
 constexpr int M = 16;
 
 __device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < INFINITY; }
@@ -51,7 +52,7 @@ __device__ __forceinline__ uint32_t v_at(int c, int lm, int g, uint32_t stride) 
   return (kt * M + score_key<M>(t, g)) * stride + 4 * (lm * 4 + c % T::VP * 4 * M);
 }
 
-// RG groups of 16 rows a workgroup.
+// RG groups of 16 rows a row set.
 template <int D, int RG>
 __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2)))
     packed_f32_kernel(const PackedArgs a) {
@@ -70,18 +71,29 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
   const int unit = divide((int)blockIdx.x, a.by_H_kv);
   const int kvh = (int)blockIdx.x - unit * a.H_kv;
   const PackedItem it = a.items[unit];
-  if (!inside(a, it, ROWS)) return;
+  const int by = it.split & 3;  // 2^by waves share a row set
+  const int KS = 1 << by;
+  if (!inside(a, it, ROWS * kWaves >> by)) return;
   const int G = a.G;
   const int n = it.keys;
-  const int S = (n + CK - 1) / CK;
+  const int set = w >> by, part = w & (KS - 1);
+  const int first = set * ROWS;  // this wave's rows, from the unit's first on
+  const int used = it.rows - first < ROWS ? it.rows - first : ROWS;
+  // keys that every row of the wave sees, sub-tiles that some row does
+  int whole = 0, S = 0;
+  if (used > 0) {
+    const int lo = it.seen + divide(it.head0 + first, a.by_G);
+    const int hi = it.seen + divide(it.head0 + first + used - 1, a.by_G);
+    whole = lo < n ? lo : n;
+    S = ((hi < n ? hi : n) + CK - 1) / CK;
+  }
 
   f32x4_t qr[RG * T::QI];
   int left[RG];  // keys this lane's row of each group sees
   bool valid[RG];
-  const int whole = it.seen < n ? it.seen : n;  // keys that every row of the unit sees
 #pragma unroll
   for (int rg = 0; rg < RG; ++rg) {
-    const int r = rg * M + lm;
+    const int r = first + rg * M + lm;
     valid[rg] = r < it.rows;
     const int x = it.head0 + (valid[rg] ? r : 0);
     const int tok = divide(x, a.by_G);
@@ -150,14 +162,14 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
   {
     constexpr int NC = T::KC + T::VN;  // chunks of a sub-tile
     f32x4_t ring[kLead];
-    __amdgpu_buffer_rsrc_t krs = sub_rsrc<D>(kb, ks, w, n);
-    if (w < S) {
+    __amdgpu_buffer_rsrc_t krs = sub_rsrc<D>(kb, ks, part, n);
+    if (part < S) {
 #pragma unroll
       for (int c = 0; c < kLead; ++c) ring[c] = load4(krs, k_at<D>(c, lm, g, ks));
     }
-    for (int x = w; x < S; x += kWaves) {
+    for (int x = part; x < S; x += KS) {
       const __amdgpu_buffer_rsrc_t vrs = sub_rsrc<D>(vb, vs, x, n);
-      const __amdgpu_buffer_rsrc_t next = sub_rsrc<D>(kb, ks, x + kWaves, n);  // past the end: zeros
+      const __amdgpu_buffer_rsrc_t next = sub_rsrc<D>(kb, ks, x + KS, n);  // past the end: zeros
       auto issue = [&](int c) {
         const int y = c + kLead;
         if (y < T::KC)
@@ -198,7 +210,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
           bad = __builtin_fmaf(valid[rg] ? o[rg][b][t] : 0.f, 0.f, bad);
     if (__ballot(bad != 0.f) != 0) {
       clear();
-      for (int x = w; x < S; x += kWaves) {
+      for (int x = part; x < S; x += KS) {
         const __amdgpu_buffer_rsrc_t krs = sub_rsrc<D>(kb, ks, x, n), vrs = sub_rsrc<D>(vb, vs, x, n);
         const bool all = whole >= CK * (x + 1);
         f32x4_t ring[kLead];
@@ -269,53 +281,57 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
         opart[at * LD + 4 * (b / 4 * M + score_key<M>(t, g)) + b % 4] = o[rg][b][t];
   }
   __syncthreads();
-  auto merged = [&](int row, float* wgt) -> double {  // sum of row `row`, weight of each wave
-    float mm = kNegBig;
+  // where row r's state of the first of its waves lies
+  auto state = [&](int r) { return (r / ROWS << by) * ROWS + r % ROWS; };
+  const int all = ROWS * kWaves >> by, rows = it.rows < all ? it.rows : all;
+  if (tid < rows) {
+    // the weight of each wave takes its max's place, what the sum is divided by the first sum's
+    const int at = state(tid);
+    float mw[kWaves], mm = kNegBig;
 #pragma unroll
-    for (int y = 0; y < kWaves; ++y) mm = fmaxf(mm, mpart[y * ROWS + row]);
+    for (int y = 0; y < kWaves; ++y)
+      if (y < KS) mm = fmaxf(mm, mw[y] = mpart[at + y * ROWS]);
     double lt = 0.0;
 #pragma unroll
-    for (int y = 0; y < kWaves; ++y) {
-      wgt[y] = fast_exp2(mpart[y * ROWS + row] - mm);
-      lt += lpart[y * ROWS + row] * (double)wgt[y];
-    }
-    wgt[kWaves] = mm;
-    return lt;
-  };
-  const int rows = it.rows;
-  float wgt[kWaves + 1];
-  if (tid < ROWS && tid < rows) {
-    const float lf = (float)merged(tid, wgt);
+    for (int y = 0; y < kWaves; ++y)
+      if (y < KS) {
+        const float wgt = fast_exp2(mw[y] - mm);
+        lt += lpart[at + y * ROWS] * (double)wgt;
+        mpart[at + y * ROWS] = wgt;
+      }
+    const float lf = (float)lt;
+    lpart[at] = it.part >= 0 ? 1.f : (lf == 0.f ? 0.f : 1.0f / lf);
     if (it.part >= 0) {
-      const int64_t at = (int64_t)(it.part + tid) * a.H_kv + kvh;
-      *reinterpret_cast<f32x2_t*>(a.part_ml + 2 * at) = f32x2_t{wgt[kWaves], lf};
+      const int64_t to = (int64_t)(it.part + tid) * a.H_kv + kvh;
+      *reinterpret_cast<f32x2_t*>(a.part_ml + 2 * to) = f32x2_t{mm, lf};
     } else if (a.lse != nullptr) {
       const int row = it.head0 + tid, tok = divide(row, a.by_G);
       a.lse[(int64_t)(kvh * G + (row - tok * G)) * a.lse_head + it.q_row + tok] =
-          lf == 0.f ? -INFINITY : (wgt[kWaves] + __log2f(lf)) * kLn2;
+          lf == 0.f ? -INFINITY : (mm + __log2f(lf)) * kLn2;
     }
   }
-  for (int idx = tid; idx < ROWS * D / 4; idx += NT) {
+  __syncthreads();
+#pragma unroll 2
+  for (int idx = tid; idx < rows * D / 4; idx += NT) {
     const int r = idx / (D / 4), d4 = (idx % (D / 4)) * 4;
-    if (r >= rows) break;
-    const float lf = (float)merged(r, wgt);
+    const int at = state(r);
+    const float inv = (float)lpart[at];
     f32x4_t acc = f32x4_t{};
 #pragma unroll
-    for (int y = 0; y < kWaves; ++y) {
-      const f32x4_t p = *reinterpret_cast<const f32x4_t*>(opart + (y * ROWS + r) * LD + d4);
+    for (int y = 0; y < kWaves; ++y)
+      if (y < KS) {
+        const float wgt = mpart[at + y * ROWS];
+        const f32x4_t p = *reinterpret_cast<const f32x4_t*>(opart + (at + y * ROWS) * LD + d4);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = fmaf(p[e], wgt[y], acc[e]);
-    }
-    if (it.part >= 0) {
-      *reinterpret_cast<f32x4_t*>(a.part_o + ((int64_t)(it.part + r) * a.H_kv + kvh) * D + d4) = acc;
-      continue;
-    }
-    const float inv = lf == 0.f ? 0.f : 1.0f / lf;
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(p[e], wgt, acc[e]);
+      }
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] *= inv;
     const int row = it.head0 + r, tok = divide(row, a.by_G);
-    float* const op = static_cast<float*>(a.o) + (it.q_row + tok) * a.ot +
-                      (int64_t)(kvh * G + (row - tok * G)) * a.oh;
+    float* const op = it.part >= 0
+                          ? a.part_o + ((int64_t)(it.part + r) * a.H_kv + kvh) * D
+                          : static_cast<float*>(a.o) + (it.q_row + tok) * a.ot +
+                                (int64_t)(kvh * G + (row - tok * G)) * a.oh;
     *reinterpret_cast<f32x4_t*>(op + d4) = acc;
   }
 }

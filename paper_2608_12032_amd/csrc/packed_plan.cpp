@@ -45,6 +45,23 @@ int tile_part_keys(bool bf16, int64_t rows, int k_len) {
   return ((k_len + parts - 1) / parts + step - 1) / step * step;
 }
 
+// fp32: binary logarithm of the waves that share a row set: no more than there are 32-key
+// sub-tiles, so that none idles and few states are merged.  us, all eight / these, dense,
+// d = 64: 8,192 x 12 heads over 32 keys 85 / 24, over 64 88 / 36, over 128 93 / 65; but 300
+// x 4, where few workgroups are left, 6.3 / 8.3, 6.5 / 8.2, 6.9 / 8.0.  With two sub-tiles a
+// wave 128 keys took 49 and 10.3, 256 keys (121 and 8.3 with eight) 91 and 10.1.
+constexpr int kAllWaves = 3;
+static_assert(1 << kAllWaves == kPackedF32Waves, "a workgroup's waves");
+int key_waves(int k_len) {
+  int by = 0;
+  while (by < kAllWaves && k_len > (32 << by)) ++by;
+  return by;
+}
+// Rows of a unit of a sequence's tiles, `rows` those of a tile or row set.
+int unit_rows(bool bf16, int rows, int k_len) {
+  return bf16 ? rows : rows * kPackedF32Waves >> key_waves(k_len);
+}
+
 // fp32 units of 32 rows below which a call takes 16.  us in tiles of 16 / of 32, dense:
 // 128 units (1,024 x 4 heads, d = 128) 25.6 / 39.7; 256 47.2 / 40.2 and causal 31.7 / 40.2;
 // 555 410 / 427, at d = 64 200 / 232; 768 255 / 211, at d = 64 119 / 116.
@@ -63,14 +80,15 @@ int tile_rows(const PackedSeqs& s) {
     const int64_t rows = (int64_t)s.q_len[i] * s.G;
     if (rows <= kPackedFew[0]) continue;
     const int keys = std::max(1, tile_part_keys(false, rows, s.k_len[i]));
-    wide += (rows + kPackedTile[0] - 1) / kPackedTile[0] * std::max(1, (s.k_len[i] + keys - 1) / keys);
+    const int unit = unit_rows(false, kPackedTile[0], s.k_len[i]);
+    wide += (rows + unit - 1) / unit * std::max(1, (s.k_len[i] + keys - 1) / keys);
   }
   return wide * s.H_kv < kWideUnits ? kPackedNarrow : kPackedTile[0];
 }
 
 // Calls tile(item), few(item), join(row) for every unit, in order; returns their number.
 template <typename Tile, typename Few, typename Join>
-Counts walk(const PackedSeqs& s, int block, Tile&& tile, Few&& few, Join&& join) {
+Counts walk(const PackedSeqs& s, int tile_rows, Tile&& tile, Few&& few, Join&& join) {
   Counts c = {};
   int64_t q0 = 0, k0 = 0;
   for (int i = 0; i < s.n; ++i) {
@@ -81,9 +99,11 @@ Counts walk(const PackedSeqs& s, int block, Tile&& tile, Few&& few, Join&& join)
     const int shift = k_len - q_len;  // causal: token t sees keys up to t + shift
     const int64_t rows = (int64_t)q_len * s.G;
     if (rows == 0) continue;
+    const bool tiled = rows > kPackedFew[s.bf16];
     PackedItem it = {};
     it.part = -1;
-    const bool tiled = rows > kPackedFew[s.bf16];
+    it.split = s.bf16 ? 0 : tiled ? key_waves(k_len) : kAllWaves;
+    const int block = unit_rows(s.bf16, tile_rows, k_len);
     const int keys = tiled ? tile_part_keys(s.bf16, rows, k_len) : part_keys(s.bf16, k_len);
     const int parts = std::max(1, (int)(((int64_t)k_len + keys - 1) / std::max(1, keys)));
     if (tiled) {

@@ -97,6 +97,9 @@ CASES = [  # dtype, d, H, Hkv, causal, q_lens, k_lens
     # mixed
     (BF, 128, 4, 2, True, (0, 1, 600, 3, 0, 17, 64), (4, 900, 600, 3, 0, 2100, 64)),
     (F, 128, 2, 2, False, (1, 15, 16, 17, 31, 32, 33, 150), (1, 31, 32, 33, 255, 256, 257, 300)),
+    # few keys: 1, 2, 4 or 8 waves to a row set
+    (F, 128, 2, 2, False, (300, 257, 150, 90, 33, 129), (32, 100, 200, 64, 33, 7)),
+    (F, 64, 6, 2, True, (64, 100, 65, 129, 31, 20), None), (F, 128, 3, 1, True, (50, 90, 30), (64, 128, 7)),
     (F, 64, 6, 2, True, (100, 1, 333, 64), None), (F, 128, 3, 1, True, (40, 130), (300, 60)),
     (F, 128, 4, 1, True, (20, 5, 64), (3001, 9000, 2048)), (F, 64, 3, 1, False, (90, 6), (2050, 7000)),
     (F, 64, 8, 2, True, (1, 4, 2, 1), (3000, 511, 513, 20_011)),
@@ -159,6 +162,20 @@ def test_a_sequence_gives_the_same_bits_alone_and_packed(L, dtype):
         o1, _ = call(L, q[a:a + x, 2:], k[b:b + y, 1:], v[b:b + y, 1:], [x], [y], True)
         assert torch.equal(o1, o[a:a + x, 2:])  # a head's group alone
         a, b = a + x, b + y
+
+
+def test_fp32_rows_give_the_same_bits_in_a_large_call(L):
+    """A call of many units takes row sets of 32 rows, a small one of 16."""
+    d, ql, kl = 64, (130, 77, 40, 90_000), (20, 60, 200, 31)
+    q = randn(sum(ql), 4, d, seed=80, dtype=F).cuda()
+    k, v = (randn(sum(kl), 2, d, seed=s, dtype=F).cuda() for s in (81, 82))
+    for causal in (False, True):
+        o, lse = call(L, q, k, v, ql, kl, causal)
+        a = b = 0
+        for x, y in zip(ql[:3], kl):
+            o1, l1 = call(L, q[a:a + x], k[b:b + y], v[b:b + y], [x], [y], causal)
+            assert torch.equal(o1, o[a:a + x]) and torch.equal(l1, lse[:, a:a + x])
+            a, b = a + x, b + y
 
 
 @pytest.mark.parametrize("dtype", [BF, F])

@@ -17,7 +17,7 @@ def L():
 
 
 ITEM = np.dtype([("q_row", "<i8"), ("k_row", "<i8"), ("head0", "<i4"), ("rows", "<i4"), ("keys", "<i4"),
-                 ("seen", "<i4"), ("part", "<i4"), ("unused", "<i4")])
+                 ("seen", "<i4"), ("part", "<i4"), ("split", "<i4")])
 JOIN = np.dtype([("q_row", "<i8"), ("in_group", "<i4"), ("part", "<i4"), ("step", "<i4"), ("n", "<i4")])
 
 
@@ -38,8 +38,8 @@ def test_units_cover_every_row_and_key_once(L, dtype, causal, seed):
     kl = [rng.choice([0, 1, 63, 128, 129, 700, 5000, 50_000]) for _ in ql]
     p = L.losa_packed_plan(ql, kl, 2 * G, 2, dtype, causal=causal, device="cpu")
     tiles, few, joins = units(p)
-    block, most = p.info.tile_rows, 32 if dtype == torch.bfloat16 else 16
-    assert block in ((128,) if dtype == torch.bfloat16 else (16, 32))
+    most = 32 if dtype == torch.bfloat16 else 16
+    assert p.info.tile_rows in ((128,) if dtype == torch.bfloat16 else (16, 32))
     assert p.q_rows == max([0] + [sum(ql[:i + 1]) for i in range(7) if ql[i]])
     parts = []
     q0 = k0 = 0
@@ -47,6 +47,11 @@ def test_units_cover_every_row_and_key_once(L, dtype, causal, seed):
         rows, shift = q * G, k - q
         sees = lambda t: max(0, min(k, t + shift + 1)) if causal else k  # noqa: E731
         mine = [x for x in (tiles if rows > most else few) if q0 <= x["q_row"] < q0 + q]
+        block = p.info.tile_rows
+        if dtype == torch.float32:  # the fewer keys, the more of a workgroup's waves have rows of their own
+            split = 3 if rows <= most else sum(k > n for n in (32, 64, 128))
+            assert all(x["split"] == split for x in mine)
+            block = block * 8 >> split
         number = lambda x: (int(x["q_row"]) - q0) * G + int(x["head0"])  # noqa: E731
         for x in mine:
             assert int(x["rows"]) == rows - number(x)
