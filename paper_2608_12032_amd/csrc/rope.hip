@@ -29,7 +29,9 @@ namespace {
 constexpr int kWaves = 4;   // waves of a workgroup
 constexpr int kUnroll = 4;  // heads in flight per lane
 // Heads up to which a wave holds a token's for their norm: no barrier, loads not
-// repeated (121 us where the workgroup's waves share them: 138).
+// repeated (121 us where the workgroup's waves share them: 138).  Up to kUnroll heads
+// take a form for those (2 heads x 32,760 x 128, fp32: 35 us, in the one for 16 heads 48),
+// and one head's is its row's.
 constexpr int kAlone = 16;
 
 // Output bytes of a call from which it is streamed: stores, and bf16 loads of 16 bytes
@@ -39,8 +41,8 @@ constexpr int kAlone = 16;
 constexpr int64_t kStreamBytes = (int64_t)32 << 20;
 
 // Whose norm: each row's; a token's, its heads over the workgroup's waves; a token's, all
-// its heads in one wave.
-enum Norm { kEach, kShared, kOwn };
+// its heads in one wave, kAlone at most or kUnroll.
+enum Norm { kEach, kShared, kOwn, kOwnFew };
 
 // Eight values of a row as they lie in memory, in two groups of four.
 template <typename T>
@@ -130,7 +132,7 @@ __device__ __forceinline__ float row_sum(float x) {
 }
 
 // Workgroup -> tensor, batch, token tile, heads.  kEach: a wave owns a tile of tokens
-// and `hc` heads, the workgroup's waves neighbouring tiles.  kOwn: the same with all of the
+// and `hc` heads, the workgroup's waves neighbouring tiles.  kOwn, kOwnFew: the same with all of the
 // 16 heads or fewer, which the wave holds in registers between their sum and their
 // output.  kShared: a workgroup owns a tile, its waves take the heads in turn and add
 // their sums in LDS; with more than 16 heads a pass reads them again.
@@ -336,6 +338,8 @@ void launch_rows_of(const RowsArgs& a, Norm whose, uint32_t groups, hipStream_t 
     hipLaunchKernelGGL((rows_kernel<T, D, HALVES, STREAM, kEach>), grid, block, 0, stream, a);
   else if (whose == kOwn)
     hipLaunchKernelGGL((rows_kernel<T, D, HALVES, STREAM, kOwn>), grid, block, 0, stream, a);
+  else if (whose == kOwnFew)
+    hipLaunchKernelGGL((rows_kernel<T, D, HALVES, STREAM, kOwnFew>), grid, block, 0, stream, a);
   else
     hipLaunchKernelGGL((rows_kernel<T, D, HALVES, STREAM, kShared>), grid, block, 0, stream, a);
 }
@@ -349,7 +353,10 @@ hipError_t launch(RowsArgs& a, int tensors, bool all, hipStream_t stream) {
     heads += a.t[i].H;
     if (a.t[i].norm != kNormNone && a.t[i].H > normed) normed = a.t[i].H;
   }
-  const Norm whose = !all || normed == 0 ? kEach : (normed <= kAlone ? kOwn : kShared);
+  const Norm whose = !all || normed <= 1 ? kEach  // (over one head it is the head's)
+                     : normed <= kUnroll ? kOwnFew
+                     : normed <= kAlone  ? kOwn
+                                         : kShared;
   const int64_t tiles = (a.n_pad + TW - 1) / TW;
   a.tiles = (int)(whose == kShared ? tiles : (tiles + kWaves - 1) / kWaves);
   for (int i = 0; i < 3; ++i) {
