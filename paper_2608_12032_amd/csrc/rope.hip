@@ -132,9 +132,9 @@ __device__ __forceinline__ float row_sum(float x) {
 }
 
 // Workgroup -> tensor, batch, token tile, heads.  kEach: a wave owns a tile of tokens
-// and `hc` heads, the workgroup's waves neighbouring tiles.  kOwn, kOwnFew: the same with all of the
-// 16 heads or fewer, which the wave holds in registers between their sum and their
-// output.  kShared: a workgroup owns a tile, its waves take the heads in turn and add
+// and `hc` heads, the workgroup's waves neighbouring tiles.  kOwn, kOwnFew: the same with
+// all of the 16 heads or fewer, which the wave holds in registers between their sum and
+// their output.  kShared: a workgroup owns a tile, its waves take the heads in turn and add
 // their sums in LDS; with more than 16 heads a pass reads them again.
 template <typename T, int D, bool HALVES, bool STREAM, Norm WHOSE>
 __global__ void __launch_bounds__(64 * kWaves) rows_kernel(const RowsArgs a) {
