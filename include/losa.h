@@ -442,7 +442,8 @@ size_t losa_packed_workspace_bytes(const losa_packed_info* info, int d);
  *             by every call.
  * Arithmetic as in losa_sparse_attn_fwd (bf16: probabilities rounded to bf16 for the
  * P V product; f32: the normaliser of a unit carried in fp64).  Values that are not
- * finite, at keys that a row does not see, do not reach it.
+ * finite, at keys that a row does not see, do not reach it.  Scores below -1e30 (scaled,
+ * in base-2 units) count as -inf.
  */
 losa_status losa_packed_attn_fwd(const losa_view* q, const losa_view* k, const losa_view* v,
                                  int64_t q_rows, int64_t k_rows, const losa_packed_info* info,
