@@ -22,6 +22,7 @@ LIB_PATH = os.environ.get("LOSA_LIBRARY") or os.path.join(_HERE, "liblosa.so")
 
 LOSA_DTYPE_F32 = 0
 LOSA_DTYPE_BF16 = 1
+_DTYPES = {torch.float32: LOSA_DTYPE_F32, torch.bfloat16: LOSA_DTYPE_BF16}
 STATUS = {0: "LOSA_OK", 1: "LOSA_ERR_NULL_POINTER", 2: "LOSA_ERR_INVALID_SHAPE",
           3: "LOSA_ERR_INVALID_TAU", 4: "LOSA_ERR_ALIGNMENT", 5: "LOSA_ERR_UNSUPPORTED",
           6: "LOSA_ERR_CAPACITY", 7: "LOSA_ERR_HIP"}
@@ -593,19 +594,47 @@ def losa_qk_norm_rope(q, k, v=None, *, norm: str | None = "rms", over: str = "he
 
 class PackedPlan:
     """Plan of a batch of packed sequences on a device: what losa_packed_plan returns.
-    ``info`` holds its sizes (losa_packed_info), ``data`` the units of work (neither to be
-    replaced)."""
+    ``info`` is a copy of its sizes (losa_packed_info), ``data`` the units of work (not to
+    be replaced)."""
 
     def __init__(self, info, data, dtype):
-        self.info, self._data, self.dtype = info, data, dtype
-        self.q_rows, self.k_rows = info.q_rows, info.k_rows
-        self.heads, self.kv_heads = info.H, info.H_kv
-        self._at = ctypes.addressof(info)
-        self._need = {d: int(lib.losa_packed_workspace_bytes(self._at, d)) for d in (64, 128)}
+        if _DTYPES.get(dtype) != info.dtype:
+            raise ValueError(f"dtype {dtype} is not the one of the plan's sizes")
+        if (data.dtype != torch.int64 or not data.is_contiguous()
+                or data.numel() * 8 < max(8, info.bytes)):
+            raise ValueError(f"data must be contiguous int64 of {info.bytes} bytes")
+        # (as bytes, which belong to this object and its copies; ctypes passes their address)
+        self._info, self._data, self._dtype = bytes(info), data, dtype
+        self._heads, self._kv_heads = info.H, info.H_kv
+        self._need = {d: int(lib.losa_packed_workspace_bytes(self._info, d)) for d in (64, 128)}
+
+    @property
+    def info(self):
+        return _PackedInfo.from_buffer_copy(self._info)
 
     @property
     def data(self):
         return self._data
+
+    @property
+    def dtype(self):
+        return self._dtype
+
+    @property
+    def heads(self):
+        return self._heads
+
+    @property
+    def kv_heads(self):
+        return self._kv_heads
+
+    @property
+    def q_rows(self):
+        return self.info.q_rows
+
+    @property
+    def k_rows(self):
+        return self.info.k_rows
 
     def workspace_bytes(self, d: int) -> int:
         return self._need.get(d, 0)
@@ -637,12 +666,11 @@ def losa_packed_plan(q_lens, k_lens, heads: int, kv_heads: int, dtype, causal: b
                 raise ValueError(f"{name} holds a length beyond 32 bits")
             x = (kind * max(n, 1))(*x)
         arrays.append(x)
-    code = LOSA_DTYPE_BF16 if dtype == torch.bfloat16 else LOSA_DTYPE_F32
     info = _PackedInfo()
 
     def call(plan, room):
-        _check(lib.losa_packed_plan(*arrays, n, code, heads, kv_heads, int(causal), plan, room,
-                                    ctypes.addressof(info)), "losa_packed_plan")
+        _check(lib.losa_packed_plan(*arrays, n, _DTYPES[dtype], heads, kv_heads, int(causal), plan,
+                                    room, ctypes.addressof(info)), "losa_packed_plan")
 
     call(None, 0)
     host = torch.empty(max(1, info.bytes // 8), dtype=torch.int64)
@@ -672,8 +700,8 @@ def losa_packed_attn_fwd(q, k, v, plan: PackedPlan, scale: float | None = None,
             raise ValueError(f"{name} must be a [rows, heads, d] tensor")
     rows, _, d = q.shape
     k_rows = k.shape[0]
-    dev, dt = q.device, plan.dtype
-    shape, shape_kv = (rows, plan.heads, d), (k_rows, plan.kv_heads, d)
+    dev, dt, heads = q.device, plan._dtype, plan._heads
+    shape, shape_kv = (rows, heads, d), (k_rows, plan._kv_heads, d)
     if not q.is_cuda:
         raise ValueError(f"q must live on a GPU (got {dev})")
     if plan._data.device != dev:
@@ -687,8 +715,8 @@ def losa_packed_attn_fwd(q, k, v, plan: PackedPlan, scale: float | None = None,
     lse_at = None
     if want_lse:
         if lse is None:
-            lse = torch.empty((plan.heads, rows), dtype=torch.float32, device=dev)
-        lse_at = _arg(lse, "lse", dev, dtype=torch.float32, shape=(plan.heads, rows)).data_ptr()
+            lse = torch.empty((heads, rows), dtype=torch.float32, device=dev)
+        lse_at = _arg(lse, "lse", dev, dtype=torch.float32, shape=(heads, rows)).data_ptr()
     need = plan.workspace_bytes(d)
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
@@ -696,7 +724,7 @@ def losa_packed_attn_fwd(q, k, v, plan: PackedPlan, scale: float | None = None,
     if workspace is not None:
         _arg(workspace, "workspace", dev, nbytes=need)
         ws_at, ws_bytes = workspace.data_ptr(), workspace.nbytes
-    st = _call(dev, lib.losa_packed_attn_fwd, qv, kv, vv, rows, k_rows, plan._at,
+    st = _call(dev, lib.losa_packed_attn_fwd, qv, kv, vv, rows, k_rows, plan._info,
                plan._data.data_ptr(), d, 1.0 / math.sqrt(d) if scale is None else scale, ov, lse_at,
                rows, ws_at, ws_bytes)
     if st:

@@ -1,6 +1,8 @@
 """The plan of the packed attention without a GPU (its units cover every row and key
 once, whatever the batch), and what the C ABI refuses before any HIP call."""
+import copy
 import ctypes
+import pickle
 import random
 
 import numpy as np
@@ -229,3 +231,46 @@ def test_binding_refuses_host_tensors(L):
         L.losa_packed_attn_fwd(q, q[:, :1], q[:, :1], p)
     with pytest.raises(TypeError, match="PackedPlan"):
         L.losa_packed_attn_fwd(q, q, q, None)
+
+
+@pytest.mark.parametrize("again", [copy.copy, copy.deepcopy, lambda p: pickle.loads(pickle.dumps(p))],
+                         ids=["copy", "deepcopy", "pickle"])
+def test_a_copied_plan_holds_its_own_sizes(L, monkeypatch, again):
+    """What a call passes as the plan's sizes is the copy's own, also once the original
+    and its memory have gone to other plans."""
+    plan = L.losa_packed_plan([4, 30], [3000, 30], 4, 2, torch.bfloat16, device="cpu")
+    want, units_of = bytes(plan.info), plan.data.clone()
+    twin = again(plan)
+    del plan
+    others = [L.losa_packed_plan([n], [n], 8, 8, torch.bfloat16, device="cpu") for n in range(1, 200)]
+    passed = []
+
+    def seen(q, k, v, q_rows, k_rows, info, *rest):  # what the library would read
+        passed.append(ctypes.string_at(info, ctypes.sizeof(L._PackedInfo)))
+        return 0
+
+    monkeypatch.setattr(L, "_call", lambda dev, fn, *args: seen(*args))
+    monkeypatch.setattr(L, "_packed_view", lambda *a: b"")
+    monkeypatch.setattr(L, "_arg", lambda t, *a, **k: t)
+    on_gpu = type("OnGpu", (torch.Tensor,), {"is_cuda": property(lambda t: True)})
+    q, k = torch.zeros(34, 4, 128).as_subclass(on_gpu), torch.zeros(3030, 2, 128)
+    L.losa_packed_attn_fwd(q, k, k, twin, out=torch.zeros(34, 4, 128))
+    assert passed == [want] and bytes(twin.info) == want and len(others) == 199
+    assert torch.equal(twin.data, units_of) and twin.workspace_bytes(128) > 0
+    assert (twin.q_rows, twin.k_rows, twin.heads, twin.kv_heads) == (34, 3030, 4, 2)
+
+
+def test_a_plan_is_what_was_planned(L):
+    """A plan's sizes and units are not replaced, and fit each other."""
+    plan = L.losa_packed_plan([4, 30], [3000, 30], 4, 2, torch.bfloat16, device="cpu")
+    for name in ("info", "data", "dtype", "q_rows", "k_rows", "heads", "kv_heads"):
+        with pytest.raises(AttributeError):
+            setattr(plan, name, getattr(plan, name))
+    plan.info.n_tiles = 1 << 20  # a copy's
+    assert plan.info.n_tiles < 100
+    for data in (plan.data[:-1], plan.data.int(), plan.data.repeat(2)[::2]):
+        with pytest.raises(ValueError, match="int64"):
+            L.PackedPlan(plan.info, data, plan.dtype)
+    with pytest.raises(ValueError, match="dtype"):
+        L.PackedPlan(plan.info, plan.data, torch.float32)
+    assert L.PackedPlan(plan.info, plan.data, plan.dtype).workspace_bytes(64) == plan.workspace_bytes(64)
