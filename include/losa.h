@@ -413,7 +413,8 @@ typedef struct {
  * q_len, k_len      int32 [n_seq], >= 0.  n_seq >= 0.
  * plan              NULL: only `info` is filled.  Else at least info->bytes bytes,
  *                   8-byte aligned.
- * H must be a multiple of H_kv.
+ * H must be a multiple of H_kv.  More units than one launch takes (2^32 threads: some 16
+ * million workgroups in bf16, 8 in f32) are refused (LOSA_ERR_INVALID_SHAPE).
  * A sequence's rows are q_len * H / H_kv per key head.  Few rows (up to 2,048 in bf16, 512
  * in f32) over many keys split the keys into parts that are joined; how follows from its
  * own lengths and H / H_kv alone, so a sequence gives the same bits alone and packed

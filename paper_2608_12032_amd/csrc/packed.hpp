@@ -84,7 +84,11 @@ __device__ __forceinline__ bool inside(const PackedArgs& a, const PackedJoin& j)
 constexpr int kPackedTile[2] = {32, 128};  // [bf16]
 constexpr int kPackedFew[2] = {16, 32};
 constexpr int kPackedNarrow = 16;
-constexpr int kPackedF32Waves = 8;
+// Waves of a workgroup: of units, of joins (a row of up to kFewParts parts a wave).
+constexpr int kPackedWaves[2] = {8, 4};  // [bf16]
+constexpr int kJoinWaves = 8;
+// Workgroups of one launch: it counts its threads in 32 bits.
+constexpr int64_t most_workgroups(int waves) { return (((int64_t)1 << 32) - 1) / (64 * waves); }
 // The sequences of a call as the plan takes them (starts null: one after another).
 struct PackedSeqs {
   const int64_t *q_start, *k_start;

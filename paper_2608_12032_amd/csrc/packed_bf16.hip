@@ -287,7 +287,7 @@ __device__ __forceinline__ RowOut part_out(const PackedArgs& a, const PackedItem
   return {at * D, 2 * at};
 }
 
-constexpr int NW = 4;  // waves of a workgroup
+constexpr int NW = kPackedWaves[1];  // waves of a workgroup
 
 // LDS of a workgroup.
 template <int D>
@@ -733,7 +733,6 @@ __global__ void __launch_bounds__(64 * NW)
 // are then merged in order.  Lane t holds the max and sum of the wave's t-th part; the
 // outputs, rescaled to the wave's max, are added in order, and their loads do not wait
 // for the weights.
-constexpr int kJoinWaves = 8;
 static_assert(kMostParts / kJoinWaves <= 64 && kFewParts <= 64, "a lane for each part of a wave");
 
 // o (un-normalised), max and sum of parts at(0) .. at(n - 1); m, f: see above.

@@ -20,7 +20,7 @@ namespace losa {
 
 namespace {
 
-constexpr int kWaves = kPackedF32Waves;  // of a workgroup: two per SIMD
+constexpr int kWaves = kPackedWaves[0];  // of a workgroup: two per SIMD
 constexpr int M = 16;
 
 __device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < INFINITY; }

@@ -51,7 +51,7 @@ int tile_part_keys(bool bf16, int64_t rows, int k_len) {
 // x 4, where few workgroups are left, 6.3 / 8.3, 6.5 / 8.2, 6.9 / 8.0.  With two sub-tiles a
 // wave 128 keys took 49 and 10.3, 256 keys (121 and 8.3 with eight) 91 and 10.1.
 constexpr int kAllWaves = 3;
-static_assert(1 << kAllWaves == kPackedF32Waves, "a workgroup's waves");
+static_assert(1 << kAllWaves == kPackedWaves[0], "a workgroup's waves");
 int key_waves(int k_len) {
   int by = 0;
   while (by < kAllWaves && k_len > (32 << by)) ++by;
@@ -59,7 +59,7 @@ int key_waves(int k_len) {
 }
 // Rows of a unit of a sequence's tiles, `rows` those of a tile or row set.
 int unit_rows(bool bf16, int rows, int k_len) {
-  return bf16 ? rows : rows * kPackedF32Waves >> key_waves(k_len);
+  return bf16 ? rows : rows * kPackedWaves[0] >> key_waves(k_len);
 }
 
 // fp32 units of 32 rows below which a call takes 16.  us in tiles of 16 / of 32, dense:
@@ -156,8 +156,11 @@ bool packed_counts(const PackedSeqs& s, PackedCounts* out) {
   out->tile_rows = tile_rows(s);
   const Counts c = walk(s, out->tile_rows, [](const PackedItem&) {}, [](const PackedItem&) {},
                         [](const PackedJoin&) {});
-  const int64_t most = ((int64_t)1 << 31) / s.H_kv - 1;
-  if (c.tiles + c.few > most || c.joins > most || c.part_rows >= ((int64_t)1 << 31))
+  // (tiles and few-row units may share a launch)
+  const int64_t units = (c.tiles + c.few) * s.H_kv;
+  const int64_t joins = c.wide * s.H_kv + ((c.joins - c.wide) * s.H_kv + kJoinWaves - 1) / kJoinWaves;
+  if (units > most_workgroups(kPackedWaves[s.bf16]) || joins > most_workgroups(kJoinWaves) ||
+      c.part_rows >= ((int64_t)1 << 31))
     return false;
   out->tiles = (int)c.tiles;
   out->few = (int)c.few;

@@ -274,3 +274,34 @@ def test_a_plan_is_what_was_planned(L):
     with pytest.raises(ValueError, match="dtype"):
         L.PackedPlan(plan.info, plan.data, torch.float32)
     assert L.PackedPlan(plan.info, plan.data, plan.dtype).workspace_bytes(64) == plan.workspace_bytes(64)
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,q_lens,k_len", [
+    (torch.bfloat16, 2, 2, [(1 << 30) - 128], 1),           # tiles, 256 threads a workgroup
+    (torch.float32, 2, 2, [(1 << 30) - 256], 1),            # 512
+    (torch.bfloat16, 16, 16, [1] * ((1 << 20) - 1), 1),     # few-row parts
+    (torch.float32, 8, 8, [1] * ((1 << 20) - 1), 1),
+    (torch.bfloat16, 2048, 64, [1] * ((1 << 15) - 1), 512),  # joins, eight rows a workgroup
+], ids=["tiles", "tiles-f32", "few", "few-f32", "joins"])
+def test_a_plan_beyond_one_launch_is_refused(L, dtype, heads, kv_heads, q_lens, k_len):
+    """A launch counts its threads in 32 bits: one unit more than fits is refused by the
+    plan, not by the launch, which may be the call's second."""
+    def status(q_lens):
+        n = len(q_lens)
+        q, k = np.array(q_lens, np.int32), np.full(n, k_len, np.int32)
+        info = L._PackedInfo()
+        st = L.lib.losa_packed_plan(None, q.ctypes.data, None, k.ctypes.data, n, L._DTYPES[dtype], heads,
+                                    kv_heads, 0, None, 0, ctypes.addressof(info))
+        if st == 0:
+            threads = 256 if dtype == torch.bfloat16 else 512
+            units = (info.n_tiles + info.n_few) * kv_heads
+            joins = info.n_wide * kv_heads + -(-(info.n_joins - info.n_wide) * kv_heads // 8)
+            assert units * threads < 1 << 32 and joins * 512 < 1 << 32
+            # the next unit is the first too many
+            assert (units + kv_heads) * threads >= 1 << 32 or joins * 512 + kv_heads * 32 * 64 >= 1 << 32
+        return st
+
+    assert status(q_lens) == 0
+    assert status([q_lens[0] + 128 * (2 if dtype == torch.float32 else 1)] if len(q_lens) == 1
+                  else q_lens + [1]) == 2
+    assert "launch" in L.lib.losa_last_error().decode()
