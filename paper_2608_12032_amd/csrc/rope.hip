@@ -368,7 +368,8 @@ hipError_t launch(RowsArgs& a, int tensors, bool all, hipStream_t stream) {
     a.blocks[i] = (int64_t)a.B * a.tiles * t.chunks;
     total += a.blocks[i];
   }
-  if (total >= ((int64_t)1 << 31)) return hipErrorInvalidConfiguration;
+  // (a launch counts its threads in 32 bits)
+  if (total * 64 * kWaves >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
   if (heads * a.B * a.n_pad * D * (int64_t)sizeof(T) >= kStreamBytes)
     launch_rows_of<T, D, HALVES, true>(a, whose, (uint32_t)total, stream);
   else

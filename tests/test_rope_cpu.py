@@ -201,3 +201,18 @@ def test_binding_refuses_host_tensors(L):
         L.losa_qk_norm_rope(x, x)
     with pytest.raises(ValueError, match="same length"):
         L.losa_rope_table((64,), (4, 4), device="cpu")
+
+
+def test_a_call_beyond_one_launch_is_refused(L):
+    """2^24 workgroups of 256 threads: a launch counts its threads in 32 bits.  (Each batch
+    takes one workgroup here; with q, k and v a third of them is enough.)"""
+    n, one = 1 << 24, dict(batch=128, token=128, head=128)
+    far = dict(one, data=FAKE + (1 << 33))
+    assert rope(L, x=view(L, **one), y=view(L, **far), B=n, N=1, N_pad=1, H=1) == 2
+    assert "more workgroups than one launch takes" in L.lib.losa_last_error().decode()
+    x = [View(FAKE + (i << 33), 128, 128, 128) for i in range(6)]
+    at = [ctypes.addressof(v) for v in x]
+    norm = norms(L)
+    assert L.lib.losa_qk_norm_rope(*at[:3], 1, n // 3 + 1, 1, 1, 1, 1, 128, ctypes.addressof(norm), None,
+                                   *at[3:], None) == 2
+    assert "more workgroups than one launch takes" in L.lib.losa_last_error().decode()
