@@ -394,6 +394,7 @@ typedef struct {
   int64_t bytes;          /* of the plan                                                   */
   int64_t q_rows, k_rows; /* rows that q and o, and k and v, must have                     */
   int64_t part_rows;      /* rows of partial results (the workspace's size)                */
+  int64_t q_run;          /* most rows of q next to each other that sequences own          */
   int32_t n_tiles, n_few;          /* units of work: tiles of tile_rows rows, parts of few  */
   int32_t n_joins, n_wide;         /* rows joined from parts, those of many parts          */
   int32_t tile_rows;
@@ -436,6 +437,8 @@ size_t losa_packed_workspace_bytes(const losa_packed_info* info, int d);
  * plan        device, 8-byte aligned, what losa_packed_plan filled together with `info`.
  * o           out, view like q: the sequences' rows.  A row that sees no key is 0.
  *             Rows that no sequence owns are left as they are.  May be q (same view).
+ *             Rows next to each other (info->q_run of them) that overlap are refused;
+ *             sequences with a gap between them are the caller's to keep apart.
  * lse         out, nullable, fp32, 4-byte aligned: natural-log logsumexp of the scaled
  *             scores of row r and head h at lse[h*lse_head + r]; -inf where no key is
  *             seen.  lse_head >= info->q_rows.

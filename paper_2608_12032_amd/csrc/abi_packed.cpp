@@ -16,30 +16,51 @@ using losa::fail;
 using losa::hip_status;
 using losa::take_view;
 
-// The two sequences of `s` that own the same row of q, if any (an index pair).
-losa_status check_disjoint(const int64_t* start, const int32_t* len, int n) {
-  if (!start || n < 2) return LOSA_OK;  // one after another
+// Refuses sequences that own the same row of q; *run: the most neighbouring rows that
+// sequences own.
+losa_status check_disjoint(const int64_t* start, const int32_t* len, int n, int64_t* run) {
+  *run = 0;
+  if (!start) {  // one after another
+    for (int i = 0; i < n; ++i) *run += len[i];
+    return LOSA_OK;
+  }
+  if (n == 0) return LOSA_OK;
   int* const by = new (std::nothrow) int[n];
   if (!by) return fail(LOSA_ERR_CAPACITY, "no host memory to order %d sequences", n);
   for (int i = 0; i < n; ++i) by[i] = i;
   std::sort(by, by + n, [&](int a, int b) { return start[a] != start[b] ? start[a] < start[b] : a < b; });
   losa_status st = LOSA_OK;
-  int64_t end = -1;
+  int64_t first = -1, end = -1;  // the present run
   int who = -1;
   for (int x = 0; x < n && st == LOSA_OK; ++x) {
     const int i = by[x];
     if (len[i] == 0) continue;
     if (start[i] < end)
       st = fail(LOSA_ERR_INVALID_SHAPE, "sequences %d and %d own the same rows of q", who, i);
+    if (start[i] != end) first = start[i];
     end = start[i] + len[i];
+    *run = std::max(*run, end - first);
     who = i;
   }
   delete[] by;
   return st;
 }
 
+// Whether two of `rows` neighbouring rows of H heads share elements: rows a apart and
+// heads b apart lie |a token - b head| apart, so for each b the two nearest a are looked at.
+bool rows_overlap(const losa_view& y, int64_t rows, int H, int d) {
+  if (rows < 2 || H < 2 || (H - 1) * y.head + d <= y.token || (rows - 1) * y.token + d <= y.head)
+    return false;
+  for (int64_t b = 1; b < H; ++b) {
+    const int64_t a = b * y.head / y.token, past = b * y.head - a * y.token;
+    if ((a > 0 && a < rows && past < d) || (a + 1 < rows && y.token - past < d)) return true;
+  }
+  return false;
+}
+
 bool info_ok(const losa_packed_info* i) {
-  return i->bytes >= 0 && i->q_rows >= 0 && i->k_rows >= 0 && i->part_rows >= 0 && i->n_tiles >= 0 &&
+  return i->bytes >= 0 && i->q_rows >= 0 && i->k_rows >= 0 && i->part_rows >= 0 &&
+         i->q_run >= 0 && i->q_run <= i->q_rows && i->n_tiles >= 0 &&
          i->n_few >= 0 && i->n_wide >= 0 && i->n_joins >= i->n_wide && i->H > 0 && i->H_kv > 0 && i->H % i->H_kv == 0 &&
          (i->dtype == LOSA_DTYPE_F32 || i->dtype == LOSA_DTYPE_BF16) &&
          (size_t)i->bytes == losa::packed_plan_bytes({i->n_tiles, i->n_few, i->n_joins, i->n_wide, i->tile_rows, i->part_rows}) &&
@@ -75,7 +96,8 @@ losa_status losa_packed_plan(const int64_t* q_start, const int32_t* q_len, const
     if (q_len[i] > 0 && qs + q_len[i] > q_rows) q_rows = qs + q_len[i];
     if (q_len[i] > 0 && k_len[i] > 0 && ks + k_len[i] > k_rows) k_rows = ks + k_len[i];
   }
-  const losa_status st = check_disjoint(q_start, q_len, n_seq);
+  int64_t q_run = 0;
+  const losa_status st = check_disjoint(q_start, q_len, n_seq, &q_run);
   if (st != LOSA_OK) return st;
   const losa::PackedSeqs s = {q_start, k_start, q_len, k_len, n_seq, H / H_kv, H_kv,
                               causal != 0, dtype == LOSA_DTYPE_BF16};
@@ -83,8 +105,8 @@ losa_status losa_packed_plan(const int64_t* q_start, const int32_t* q_len, const
   if (!losa::packed_counts(s, &c))
     return fail(LOSA_ERR_INVALID_SHAPE, "the batch has more units of work than one launch takes");
   const losa_packed_info got = {(int64_t)losa::packed_plan_bytes(c), q_rows, k_rows, c.part_rows,
-                                c.tiles, c.few, c.joins, c.wide, c.tile_rows, H, H_kv, causal != 0,
-                                dtype};
+                                q_run, c.tiles, c.few, c.joins, c.wide, c.tile_rows, H, H_kv,
+                                causal != 0, dtype};
   if (plan) {
     if ((reinterpret_cast<uintptr_t>(plan) & 7u) != 0)
       return fail(LOSA_ERR_ALIGNMENT, "plan must be 8-byte aligned");
@@ -131,6 +153,9 @@ losa_status losa_packed_attn_fwd(const losa_view* q, const losa_view* k, const l
   if ((st = take_view("o", o, &ov, el, 1, q_rows, info->H, d, true)) != LOSA_OK) return st;
   if (((qv.token | qv.head | ov.token | ov.head) >> 31) != 0)
     return fail(LOSA_ERR_INVALID_SHAPE, "q and o: strides must be below 2^31 elements");
+  if (rows_overlap(ov, info->q_run, info->H, d))
+    return fail(LOSA_ERR_INVALID_SHAPE, "o: rows overlap (token stride %lld, head stride %lld)",
+                (long long)ov.token, (long long)ov.head);
   if (info->k_rows > 0) {
     for (int i = 0; i < 2; ++i) {
       const char* const name = i == 0 ? "k" : "v";

@@ -55,8 +55,9 @@ _QK_NORM = struct.Struct("@iif4xQQQQ").pack
 class _PackedInfo(ctypes.Structure):
     """losa_packed_info"""
     _fields_ = [("bytes", ctypes.c_int64), ("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64),
-                ("part_rows", ctypes.c_int64), ("n_tiles", ctypes.c_int32),
-                ("n_few", ctypes.c_int32), ("n_joins", ctypes.c_int32), ("n_wide", ctypes.c_int32),
+                ("part_rows", ctypes.c_int64), ("q_run", ctypes.c_int64),
+                ("n_tiles", ctypes.c_int32), ("n_few", ctypes.c_int32),
+                ("n_joins", ctypes.c_int32), ("n_wide", ctypes.c_int32),
                 ("tile_rows", ctypes.c_int32), ("H", ctypes.c_int32),
                 ("H_kv", ctypes.c_int32), ("causal", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 

@@ -305,3 +305,28 @@ def test_a_plan_beyond_one_launch_is_refused(L, dtype, heads, kv_heads, q_lens, 
     assert status([q_lens[0] + 128 * (2 if dtype == torch.float32 else 1)] if len(q_lens) == 1
                   else q_lens + [1]) == 2
     assert "launch" in L.lib.losa_last_error().decode()
+
+
+@pytest.mark.parametrize("q_lens,q_starts,run", [
+    ([4, 30], None, 34), ([4, 30], [0, 100], 30), ([4, 0, 30], [30, 7, 0], 34), ([1, 1, 1], [0, 2, 4], 1),
+    ([3, 0], None, 3), ([0], [9], 0), ([2, 5, 1, 6], [20, 40, 22, 23], 9)])
+def test_longest_run_of_neighbouring_rows(L, q_lens, q_starts, run):
+    p = L.losa_packed_plan(q_lens, [3000] * len(q_lens), 4, 2, torch.bfloat16, q_starts=q_starts, device="cpu")
+    assert p.info.q_run == run
+
+
+@pytest.mark.parametrize("token,head,starts,code", [
+    # (with no workspace: 1 is the next check)
+    (128, 128, None, 2), (128, 128, [0, 5], 2), (256, 384, None, 2), (384, 512, None, 2), (136, 40 * 136, None, 1),
+    (136, 2 * 136, None, 2), (136, 33 * 136 + 128, None, 1), (136, 29 * 136, [0, 40], 2), (136, 30 * 136, [0, 40], 1),
+    (512, 128, None, 1), (128 * 7, 256, None, 1), (128 * 6, 256, None, 2), (128, 40 * 128, None, 1), (128, 34 * 128, None, 1),
+    (128, 33 * 128, None, 2)])
+def test_output_rows_that_share_memory_are_refused(L, token, head, starts, code):
+    """Rows of one run of neighbours, 34 or the longer of two, 4 heads: each pair compared."""
+    run = 34 if starts is None else 30
+    at = sorted(r * token + h * head for r in range(run) for h in range(4))
+    assert (min(b - a for a, b in zip(at, at[1:])) < 128) == (code == 2)
+    info = L.losa_packed_plan([4, 30], [3000, 30], 4, 2, torch.bfloat16, q_starts=starts, device="cpu").info
+    assert fwd(L, info=info, q_rows=80, o=view(L, token=token, head=head, data=FAKE + (1 << 30)), ws=None,
+               lse_head=80) == code
+    assert code == 1 or "overlap" in L.lib.losa_last_error().decode()
