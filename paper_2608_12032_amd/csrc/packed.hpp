@@ -67,9 +67,11 @@ struct PackedArgs {
 // written for one that does not.)
 __device__ __forceinline__ bool inside(const PackedArgs& a, const PackedItem& it, int tile) {
   const int rows = it.rows < tile ? it.rows : tile;
-  return (it.q_row >= 0) & (it.k_row >= 0) & (it.head0 >= 0) & (it.head0 < a.G) & (it.rows > 0) &
-         (it.keys >= 0) &
-         (it.q_row + divide(it.head0 + rows - 1, a.by_G) < a.q_rows) & (it.k_row + it.keys <= a.k_rows) &
+  // (rows of 62 bits: the sums below do not wrap)
+  return ((uint64_t)(it.q_row | it.k_row) >> 62 == 0) & (it.head0 >= 0) & (it.head0 < a.G) &
+         (it.rows > 0) & (it.keys >= 0) &
+         (it.q_row + divide(it.head0 + rows - 1, a.by_G) < a.q_rows) &
+         (it.k_row + it.keys <= a.k_rows) &
          ((it.part < 0) | ((int64_t)it.part + rows <= a.part_rows));
 }
 constexpr int kMostParts = 256, kFewParts = 16;

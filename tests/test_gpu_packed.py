@@ -474,3 +474,24 @@ def test_device_argument_checks(L):
         with pytest.raises(exc, match=msg):
             fn()
     assert L.losa_packed_attn_fwd(q, k, k, p).shape == q.shape
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_units_at_the_end_of_64_bits_write_nothing(L, dtype):
+    """Rows of q or k next to 2^63 in a plan: outside whatever is added to them."""
+    d, ql, kl = 128, [3, 200], [3000, 200]
+    q = randn(sum(ql), 4, d, seed=64, dtype=dtype).cuda()
+    k, v = (randn(sum(kl), 2, d, seed=s, dtype=dtype).cuda() for s in (65, 66))
+    plan = L.losa_packed_plan(ql, kl, 4, 2, dtype, causal=True)
+    good, ws = plan.data.clone(), plan.workspace(d)
+    units = 5 * (plan.info.n_tiles + plan.info.n_few)  # 40 bytes each, q_row and k_row first
+    for word in (0, 1):
+        for far in (2 ** 63 - 1, 2 ** 63 - 2, 2 ** 63 - 30):
+            print(f"[gpu-packed] unit word {word} = {far}", flush=True)
+            plan.data.copy_(good)
+            plan.data[word:units:5] = far
+            plan.data[units::3] = 2 ** 63 - 1  # joins: 24 bytes, q_row first
+            ws.zero_()
+            out, lse = torch.full_like(q, 5.0), torch.full((4, sum(ql)), 6.0, device="cuda")
+            L.losa_packed_attn_fwd(q, k, v, plan, want_lse=True, out=out, lse=lse, workspace=ws)
+            assert (out == 5).all() and (lse == 6).all() and not ws.any(), (word, far)
