@@ -335,3 +335,101 @@ def test_device_argument_checks(L):
             continue
         with pytest.raises(exc, match=msg):
             fn()
+
+
+# Calls of a layer's size: outputs of 32 MiB and more go past the caches, and a wave takes
+# several groups of four heads one after another.  Sampled tokens against 64 bits; every
+# token bitwise against calls on a few hundred tokens, which do neither.
+SLICE = 250
+
+
+def large_positions(N, T):
+    return torch.stack([torch.arange(N) % T, torch.arange(N) // T]).to(torch.int32)
+
+
+def sampled(N):
+    return torch.cat([torch.tensor([0, 1, N - 2, N - 1]),
+                      torch.randint(0, N, (40,), generator=torch.Generator().manual_seed(16))])
+
+
+LARGE_ROPE = [  # dtype, d, halves, rot, B, N, H, pad
+    ("bf16", 128, False, 128, 1, 11_003, 12, 128), ("bf16", 128, True, 96, 1, 11_003, 13, 1),
+    ("bf16", 64, True, 64, 2, 5_501, 26, 64), ("bf16", 64, False, 48, 1, 22_001, 12, 1),
+    ("f32", 128, True, 128, 1, 11_003, 13, 64), ("f32", 128, False, 64, 3, 1_801, 14, 1),
+    ("f32", 64, False, 64, 1, 11_003, 13, 128), ("f32", 64, True, 32, 1, 16_381, 9, 1)]
+
+
+@pytest.mark.parametrize("case", LARGE_ROPE, ids=lambda c: "-".join(map(str, c)))
+def test_rope_of_a_layer(L, case):
+    dtype, d, halves, rot, B, N, H, pad = case
+    print(f"[gpu-rope] {case}", flush=True)
+    tt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    n_pad = -(-N // pad) * pad
+    assert B * H * n_pad * d * tt.itemsize >= 32 << 20
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    x = torch.randn(B, N, 2 * H, d, generator=gen, device="cuda").to(tt)[:, :, H:]
+    dims, lens = (rot // 2, rot // 2), (101, N // 101 + 1)
+    pos, t = large_positions(N, 101), L.losa_rope_table(dims, lens)
+    pos[:, N // 3:N // 3 + 77] = -1
+    pg, pairing = pos.cuda(), "halves" if halves else "interleaved"
+    y = L.losa_rope(x, t, pg, n_pad=n_pad, pairing=pairing)
+    at = sampled(N)
+    xs = x[:, at.cuda()].double().cpu()
+    ref, size = turn(xs, xs.abs(), dims, lens, pos[:, at], halves, 10000.0)
+    check(y[:, :, at.cuda()], ref, size, len(at), H)
+    assert not y[:, :, N:].any()
+    for a in range(0, N, SLICE):
+        s = slice(a, min(N, a + SLICE))
+        small = L.losa_rope(x[:, s], t, pg[:, s].contiguous(), pairing=pairing)
+        assert torch.equal(y[:, :, s], small), a
+    z = x.contiguous()  # in place
+    L.losa_rope(z, t, pg, pairing=pairing, out=z.transpose(1, 2))
+    assert torch.equal(z.transpose(1, 2), y[:, :, :N])
+
+
+LARGE_NORM = [  # dtype, d, kind, over, halves, B, N, H, Hkv, pad
+    ("bf16", 128, "rms", "head", False, 1, 9_001, 12, 12, 128), ("bf16", 64, "layer", "head", True, 2, 4_603, 24, 8, 1),
+    ("bf16", 128, "layer", "all", False, 1, 9_001, 12, 6, 64), ("bf16", 64, "rms", "all", True, 1, 22_001, 16, 4, 1),
+    ("bf16", 128, "layer", "all", True, 1, 4_603, 40, 40, 64), ("bf16", 128, "rms", "all", False, 2, 11_003, 4, 1, 1),
+    ("f32", 128, "layer", "head", True, 1, 4_603, 12, 6, 64), ("f32", 64, "rms", "head", False, 1, 9_001, 13, 13, 1),
+    ("f32", 128, "rms", "all", True, 1, 4_603, 12, 3, 128), ("f32", 64, "layer", "all", False, 1, 4_603, 17, 17, 1),
+    ("f32", 128, "layer", "all", False, 1, 9_001, 4, 2, 1)]
+
+
+@pytest.mark.parametrize("case", LARGE_NORM, ids=lambda c: "-".join(map(str, c)))
+def test_qk_norm_rope_of_a_layer(L, case):
+    dtype, d, kind, over, halves, B, N, H, Hkv, pad = case
+    print(f"[gpu-qknorm] {case}", flush=True)
+    tt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    n_pad = -(-N // pad) * pad
+    assert B * (H + 2 * Hkv) * n_pad * d * tt.itemsize >= 32 << 20
+    gen = torch.Generator(device="cuda").manual_seed(18)
+    x = torch.randn(B, N, H + 2 * Hkv, d, generator=gen, device="cuda")
+    x = (x * (1 + randn(d, seed=19).abs()).cuda() + 0.5 * randn(d, seed=20).cuda()).to(tt)
+    cut = lambda t: (t[:, :, :H], t[:, :, H:H + Hkv], t[:, :, H + Hkv:])  # noqa: E731
+    span = [h * d if over == "all" else d for h in (H, Hkv)]
+    qw, kw = 1 + 0.3 * randn(span[0], seed=21), 1 + 0.3 * randn(span[1], seed=22)
+    qb = 0.2 * randn(span[0], seed=23) if kind == "layer" else None
+    dims, lens = (d // 2, d // 4), (101, N // 101 + 1)
+    pos, t = large_positions(N, 101), L.losa_rope_table(dims, lens)
+    pg = pos.cuda()
+    args = dict(norm=kind, over=over, q_weight=qw.cuda(), k_weight=kw.cuda(),
+                q_bias=None if qb is None else qb.cuda(), eps=1e-5, table=t,
+                pairing="halves" if halves else "interleaved")
+    got = L.losa_qk_norm_rope(*cut(x), pos=pg, n_pad=n_pad, **args)
+    at = sampled(N)
+    q, k, v = (p[:, at.cuda()].double().cpu() for p in cut(x))
+    for g, part, w, b, h in ((got[0], q, qw, qb, H), (got[1], k, kw, None, Hkv)):
+        y, size = normed(part, kind, over, w, b, 1e-5)
+        ref, size = turn(y, size, dims, lens, pos[:, at], halves, 10000.0)
+        check(g[:, :, at.cuda()], ref, size, len(at), h)
+    assert torch.equal(got[2][:, :, :N], cut(x)[2].transpose(1, 2))
+    assert not any(g[:, :, N:].any() for g in got)
+    for a in range(0, N, SLICE):
+        s = slice(a, min(N, a + SLICE))
+        small = L.losa_qk_norm_rope(*cut(x[:, s]), pos=pg[:, s].contiguous(), **args)
+        assert all(torch.equal(g[:, :, s], z) for g, z in zip(got, small)), a
+    parts = cut(x.clone())  # in place
+    L.losa_qk_norm_rope(*parts, pos=pg, q_out=parts[0].transpose(1, 2), k_out=parts[1].transpose(1, 2),
+                        v_out=parts[2].transpose(1, 2), **args)
+    assert all(torch.equal(p.transpose(1, 2), g[:, :, :N]) for p, g in zip(parts, got))
