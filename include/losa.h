@@ -39,7 +39,8 @@
  *   Sec. 5.1: 128-row query blocks, 32-key key blocks).  Other valid
  *   combinations return LOSA_ERR_UNSUPPORTED.
  * - Calls are deterministic: the same inputs give bitwise identical outputs, and
- *   a head gives the same bits alone and among other heads.
+ *   a head gives the same bits alone and among other heads (losa_packed_attn_fwd: a
+ *   key head together with its query heads; a norm over all heads: a token).
  * - Memory.  An output shares no memory with another output, the workspace or an
  *   input, except o with q (the same address), and bf16 o of the path with v (anywhere).  An
  *   o over k, or over v in f32, is not detected: rows still to come would read
@@ -405,8 +406,9 @@ typedef struct {
 /*
  * The plan of a batch of packed sequences: its units of work, longest first.  A HOST
  * function (no HIP call): the arrays and `plan` are host memory.  Copy the plan to
- * the device and keep it as long as the lengths stay: every layer and step reads the
- * same one.
+ * the device and keep it as long as the lengths stay: every layer, and every step with
+ * these lengths, reads the same one.  A step that adds a token to its caches has other
+ * lengths and takes a new plan, and a captured graph keeps those it was captured with.
  *
  * q_start, k_start  int64 [n_seq], NULL: one sequence after another.  Rows of q that
  *                   two sequences own are refused (LOSA_ERR_INVALID_SHAPE); rows of k

@@ -5,6 +5,12 @@
 //   O = sum_j softmax_j(scale q . k_j) v_j over the keys j it sees (causal:
 //   j <= i + k_len - q_len), by the online softmax: running max, sum and O^T.
 //
+// Rounding.  Probabilities are rounded to bf16 for P V, the operand type of the matrix
+// instruction (in two parts they would double that product, and the matrix cores and the
+// instructions around them bound the tiles); their sum is taken before that, in fp32.
+// Relative error of O against 64 bits 1.1e-3 to 2.3e-3; rounding O alone gives 0.9e-3 to
+// 1.7e-3, plain arithmetic with such probabilities 1.1e-3 to 2.1e-3.
+//
 // Work unit.  A workgroup of four waves owns a tile of 128 rows, 32 a wave, of one sequence
 // and key head and walks a range of its keys.  Rows are numbered token * G + head in group, so a tile's rows
 // share their keys whatever G is: G heads of one token fill a tile where each alone

@@ -299,6 +299,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
         lt += lpart[at + y * ROWS] * (double)wgt;
         mpart[at + y * ROWS] = wgt;
       }
+    // (in fp32 from here on: half a step, 2^-24, of a sum of positive terms, also of a part's)
     const float lf = (float)lt;
     lpart[at] = it.part >= 0 ? 1.f : (lf == 0.f ? 0.f : 1.0f / lf);
     if (it.part >= 0) {

@@ -21,17 +21,19 @@ int part_keys(bool bf16, int k_len) {
   return (int)(keys < least ? least : keys);
 }
 
-// Keys of a part of a sequence whose rows fill up to 16 tiles: all of them, but where they
-// are many (a chunk of a prompt, drafted tokens, over a long cache), a walk that would
-// leave most CUs idle.  A part costs its rows' partial results once more, written and
-// read: the more rows, the more keys it takes.  us, whole / split, one sequence and eight
-// (fp32 four), causal, d = 128:
+// Keys of a part of a sequence's tiles.  Above 16 tiles: all of them, so a call of few heads
+// lasts as long as its longest tile (one head, 3,264 tokens causal, d = 128: 52 us, 3.3 MB).
+// Up to 16 tiles: all of them, but where they are many (a chunk of a prompt, drafted tokens,
+// over a long cache), a walk that would leave most CUs idle.  A part costs its rows' partial
+// results once more, written and read: the more rows, the more keys it takes.  us, whole /
+// split, one sequence and eight (fp32 four), causal, d = 128:
 //   bf16, 32 / 4 heads, 7 tokens over 4,096 keys 65 / 17, 66 / 22; 32,768 470 / 27, 479 / 121
 //   32 / 8 heads, 256 tokens over 4,096 keys 68 / 49, 124 / 158; 32,768 488 / 161, 977 / 1,026
 //   512 tokens over 32,768 keys 490 / 281, 1,920 / 1,998
 //   fp32, 12 / 4 heads, 64 tokens over 2,048 keys 45 / 24, 50 / 53; 32,768 570 / 142, 658 / 464
 // and with 512 keys a part at least 256 tokens over 2,048 keys took 31 and 120 (whole 38
-// and 68).
+// and 68).  The rule does not see the batch, so that a sequence gives the same bits in any:
+// eight chunks that fill the chip by themselves are up to 27 % slower for being split.
 constexpr int kSplitTiles = 16;
 int tile_part_keys(bool bf16, int64_t rows, int k_len) {
   const int block = kPackedTile[bf16];
@@ -48,8 +50,11 @@ int tile_part_keys(bool bf16, int64_t rows, int k_len) {
 // fp32: binary logarithm of the waves that share a row set: no more than there are 32-key
 // sub-tiles, so that none idles and few states are merged.  us, all eight / these, dense,
 // d = 64: 8,192 x 12 heads over 32 keys 85 / 24, over 64 88 / 36, over 128 93 / 65; but 300
-// x 4, where few workgroups are left, 6.3 / 8.3, 6.5 / 8.2, 6.9 / 8.0.  With two sub-tiles a
-// wave 128 keys took 49 and 10.3, 256 keys (121 and 8.3 with eight) 91 and 10.1.
+// x 4, where few workgroups are left, 6.3 / 8.3, 6.5 / 8.2, 6.9 / 8.0.  More sub-tiles a wave
+// gain in large calls and lose in small ones, which this rule does not tell apart: one / two
+// / four, 128 keys 65 / 49 / 45 and 8.0 / 10.3 / 14.7, 256 keys 121 / 91 / 78 and 8.3 / 10.1 /
+// 14.5; causal 256 tokens, 64 / 8 heads, eight sequences 143 / 99 / 76, two of 8 heads 8.7 /
+// 10.3 / 14.8.  Kept is what the small calls want.
 constexpr int kAllWaves = 3;
 static_assert(1 << kAllWaves == kPackedWaves[0], "a workgroup's waves");
 int key_waves(int k_len) {

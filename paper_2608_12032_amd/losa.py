@@ -650,7 +650,9 @@ def losa_packed_plan(q_lens, k_lens, heads: int, kv_heads: int, dtype, causal: b
                      q_starts=None, k_starts=None, device="cuda") -> PackedPlan:
     """Plan of sequences of ``q_lens`` query tokens over ``k_lens`` keys (None: the same),
     one after another in q and k or at ``q_starts`` and ``k_starts``.  Lengths and starts
-    are host integers.  Keep the plan for every layer and step with these lengths."""
+    are host integers.  Keep the plan for every layer and step with these lengths; caches
+    that grow by a token take a new one each time (its copy to the device waits for it), and
+    a captured graph keeps the lengths of its plan."""
     if dtype not in (torch.bfloat16, torch.float32):
         raise TypeError(f"unsupported dtype {dtype}")
     q_lens = [int(x) for x in q_lens]
